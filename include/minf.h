@@ -252,6 +252,113 @@ minf_status minf_vs_bs_attn(const minf_qkv *x, const int32_t *vs_heads, int32_t 
 minf_status minf_dense_attn(const minf_qkv *x, const int32_t *heads, int32_t n_heads,
                             void *hip_stream);
 
+/*
+ * The keys and values behind the prefill: decoding against a KV cache.
+ *
+ *   k, v    [batch, n_kv_heads, capacity, head_dim] bf16 (the prefill's K and V
+ *           may be such a cache as they are); strides in elements for (batch,
+ *           head, token), any layout the prefill calls take
+ *   lens    [batch] int32: tokens that each sequence holds, in the slots
+ *           0 .. lens[b]-1.  Device memory, read when the kernels run; values
+ *           outside [0, capacity] are taken as the nearer of the two.  Slots
+ *           behind are never read.
+ *   weight  [batch, n_kv_heads, capacity] fp32, slots contiguous, or NULL:
+ *           attention weight that every slot has received
+ *
+ * General rules as above, with these differences: capacity and lens need not
+ * be multiples of anything; the calls take every head of the layer; the
+ * sequences of a batch may run at the same time in any order.  A value in a slot
+ * that the mask hides from a row (NaN and infinities too) does not reach that
+ * row.  Results are the same bits from call to call; the sums of a sequence are
+ * cut by the lengths of the whole batch, so that its bits may differ in another
+ * batch.
+ */
+#define MINF_MAX_NEW 64   /* new tokens per call and sequence */
+
+typedef struct {
+  void *k, *v;
+  float *weight;
+  int32_t *lens;
+  int64_t k_stride[3], v_stride[3]; /* batch, head, token                          */
+  int64_t weight_stride[2];         /* batch, head                                 */
+  int32_t batch, n_kv_heads, capacity, head_dim;
+} minf_kv_cache;
+
+/*
+ * Query rows of the n_new newest tokens of every sequence: q, o [batch,
+ * n_q_heads, n_new, head_dim] bf16.  Row t of sequence b stands at position
+ * lens[b] - n_new + t (its own key is in the cache already); where that is
+ * negative there is no token, and the row gives zeros.  o may be q itself;
+ * otherwise it must not lie over anything the call reads, and no two of its
+ * rows over each other (MINF_ERR_SHAPE for strides that make them).
+ */
+typedef struct {
+  const void *q;
+  void *o;
+  int64_t q_stride[3], o_stride[3]; /* batch, head, token                          */
+  int32_t n_q_heads, n_new;
+  float softmax_scale;              /* 0 -> 1/sqrt(head_dim)                       */
+} minf_queries;
+
+typedef enum {
+  MINF_WEIGHTS_NONE = 0,
+  MINF_WEIGHTS_SET = 1,   /* weight[b, h, j]  = sum of p_ij                        */
+  MINF_WEIGHTS_ADD = 2    /* weight[b, h, j] += sum of p_ij                        */
+} minf_weights;
+
+/* Workspace sizes in bytes (0 on invalid arguments).  With weights the logits are kept, 4 bytes
+ * per query row and visible key; without them the size depends on the rows alone.  ws must be
+ * 256-byte aligned; its contents mean nothing before and after a call.  Calls that may overlap in
+ * time need a workspace each. */
+size_t minf_cache_attn_workspace_bytes(const minf_queries *x, const minf_kv_cache *cache, int32_t n_init,
+                                       int32_t n_local, int32_t weights);
+size_t minf_prefix_attn_workspace_bytes(const minf_queries *x, const minf_kv_cache *prefix,
+                                        const minf_kv_cache *cache);
+size_t minf_cache_evict_workspace_bytes(const minf_kv_cache *cache, int32_t keep);
+
+/*
+ * Attention of the new tokens with the A-shape mask (sliding window and a few
+ * first tokens that stay visible), element exact: the row at position i sees
+ * slot j iff j <= i and (j < n_init or i - j < n_local).  n_init >= 0,
+ * n_local >= 1; n_init = 0, n_local >= capacity is causal attention over the
+ * whole cache.  1 <= n_new <= MINF_MAX_NEW.
+ * weights: with MINF_WEIGHTS_SET or _ADD the call also gives every slot j <
+ * lens[b] of cache->weight the attention weight p_ij it received in this call,
+ * summed over the rows and the query heads of the K/V head's group (0 for slots
+ * that no row sees).  fp32 logits and sums in a fixed order.
+ */
+minf_status minf_cache_attn(const minf_queries *x, const minf_kv_cache *cache, int32_t n_init, int32_t n_local,
+                            int32_t weights, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Attention of a batch whose sequences share a long prefix, which is read once
+ * for all of them.  prefix: batch = 1, with the K/V heads of the cache; the row
+ * at position i of a sequence sees every slot of the prefix and the slots j <= i
+ * of its own cache.  Rows without a token give zeros, also here.  The weight
+ * arrays are not used.
+ */
+minf_status minf_prefix_attn(const minf_queries *x, const minf_kv_cache *prefix, const minf_kv_cache *cache,
+                             void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Eviction by accumulated attention weight.  Of every sequence and K/V head the
+ * first n_init slots, the last n_recent ones and, of the others, those of the
+ * largest cache->weight stay: keep in all, or all where lens[b] <= keep (ties to
+ * the lower slot; NaN counts as the smallest).  Their rows of K, V and weight
+ * move, in ascending order, to the slots 0, 1, ... of `to`; to->lens[b] =
+ * min(lens[b], keep); to->weight is 0 in the slots behind up to its capacity.
+ * Rows of to->k and to->v behind the kept ones are left as they are.
+ * kept [batch, n_kv_heads, keep] int32 (device) receives the old slots,
+ * ascending, -1 behind them.
+ * `to` is either the cache itself (the same k, v, weight and strides: eviction
+ * in place) or memory that none of the cache's k, v and weight lies in; to->lens
+ * may be cache->lens.  to->batch and to->n_kv_heads as in the cache, to->capacity
+ * >= keep (in place: the cache's); n_init, n_recent >= 0, 1 <= keep, n_init +
+ * n_recent <= keep.
+ */
+minf_status minf_cache_evict(const minf_kv_cache *cache, int32_t n_init, int32_t n_recent, int32_t keep,
+                             const minf_kv_cache *to, int32_t *kept, void *ws, size_t ws_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

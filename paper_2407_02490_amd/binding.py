@@ -16,6 +16,8 @@ __all__ = [
     "minf_build_vs_index", "minf_build_vs_index_noalloc", "minf_vs_index_from_lines", "minf_build_bs_index", "minf_ashape_attn", "minf_vs_attn", "minf_vs_bs_attn",
     "minf_bs_attn", "minf_dense_attn", "minf_vs_cover_words",
     "minf_vs_index_workspace_bytes", "minf_bs_index_workspace_bytes",
+    "KVCache", "alloc_kv_cache", "minf_cache_attn", "minf_prefix_attn", "minf_cache_evict",
+    "minf_cache_attn_workspace_bytes", "minf_prefix_attn_workspace_bytes", "minf_cache_evict_workspace_bytes",
 ]
 
 BLOCK = 64
@@ -50,6 +52,19 @@ class _VSIndex(ctypes.Structure):
 class _BSIndex(ctypes.Structure):
     _fields_ = [("blk_idx", ctypes.c_void_p), ("blk_cnt", ctypes.c_void_p), ("order", ctypes.c_void_p),
                 ("topk", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
+class _KVCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3), ("weight_stride", ctypes.c_int64 * 2),
+                ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class _Queries(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("o", ctypes.c_void_p), ("q_stride", ctypes.c_int64 * 3),
+                ("o_stride", ctypes.c_int64 * 3), ("n_q_heads", ctypes.c_int32), ("n_new", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float)]
 
 
 def lib():
@@ -89,6 +104,19 @@ def lib():
     L.minf_bs_attn.argtypes = [pq, pi, i32, ctypes.POINTER(_BSIndex), vp]
     L.minf_vs_bs_attn.restype = ctypes.c_int
     L.minf_vs_bs_attn.argtypes = [pq, pi, i32, ctypes.POINTER(_VSIndex), pi, i32, ctypes.POINTER(_BSIndex), vp]
+    pc, px = ctypes.POINTER(_KVCache), ctypes.POINTER(_Queries)
+    L.minf_cache_attn_workspace_bytes.restype = sz
+    L.minf_cache_attn_workspace_bytes.argtypes = [px, pc, i32, i32, i32]
+    L.minf_prefix_attn_workspace_bytes.restype = sz
+    L.minf_prefix_attn_workspace_bytes.argtypes = [px, pc, pc]
+    L.minf_cache_evict_workspace_bytes.restype = sz
+    L.minf_cache_evict_workspace_bytes.argtypes = [pc, i32]
+    L.minf_cache_attn.restype = ctypes.c_int
+    L.minf_cache_attn.argtypes = [px, pc, i32, i32, i32, vp, sz, vp]
+    L.minf_prefix_attn.restype = ctypes.c_int
+    L.minf_prefix_attn.argtypes = [px, pc, pc, vp, sz, vp]
+    L.minf_cache_evict.restype = ctypes.c_int
+    L.minf_cache_evict.argtypes = [pc, i32, i32, i32, pc, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -299,3 +327,124 @@ def minf_vs_bs_attn(q, k, v, o, vs_heads, vs_idx, bs_heads, bs_idx, scale=0.0, s
     hb, nb = _heads(bs_heads)
     sv, sb = vs_idx.c_struct(), bs_idx.c_struct()
     _check(lib().minf_vs_bs_attn(ctypes.byref(x), hv, nv, ctypes.byref(sv), hb, nb, ctypes.byref(sb), _stream(stream)))
+
+
+# ---------------------------------------------------------------- cache calls
+class KVCache:
+    """Keys and values of a batch of sequences, with their lengths (see minf_kv_cache): k, v
+    [B, Hkv, capacity, 128] bf16 in any strides with head_dim contiguous, or [Hkv, capacity, 128]
+    (one sequence); lens [B] int32; weight [B, Hkv, capacity] float32 (without B as k) or None.
+    Keeps the tensors; copies nothing.  K and V of a prefill are such a cache as they are."""
+
+    def __init__(self, k, v, lens, weight=None):
+        self.k, self.v, self.lens, self.weight = k, v, lens, weight
+
+    def _args(self):
+        batch = self.k.shape[0] if self.k.dim() == 4 else 1
+        return batch, self.k.shape[-3], self.k.shape[-2]
+
+    @property
+    def batch(self):
+        return self._args()[0]
+
+    @property
+    def capacity(self):
+        return self._args()[2]
+
+    def c_struct(self):
+        batch, heads, cap = self._args()
+        k, v, lens, w = self.k, self.v, self.lens, self.weight
+        assert k.dim() in (3, 4) and k.shape == v.shape, "k and v: [B, Hkv, capacity, 128] or [Hkv, capacity, 128]"
+        for t in (k, v):
+            assert t.dtype == torch.bfloat16 and t.stride(-1) == 1, "bf16, head_dim contiguous"
+        assert lens.dtype == torch.int32 and lens.shape == (batch,) and lens.is_contiguous(), "lens: int32 [B]"
+        for t in (v, lens) + (() if w is None else (w,)):
+            assert t.device == k.device, "one device"
+        s = _KVCache()
+        s.k, s.v, s.lens = k.data_ptr(), v.data_ptr(), lens.data_ptr()
+        s.k_stride[:], s.v_stride[:] = _strides4(k)[0], _strides4(v)[0]
+        if w is not None:
+            assert w.dtype == torch.float32 and w.shape == k.shape[:-1] and w.stride(-1) == 1, \
+                "weight: float32 [B, Hkv, capacity], slots contiguous"
+            s.weight = w.data_ptr()
+            s.weight_stride[:] = (0, w.stride(0)) if w.dim() == 2 else (w.stride(0), w.stride(1))
+        s.batch, s.n_kv_heads, s.capacity, s.head_dim = batch, heads, cap, k.shape[-1]
+        return s
+
+
+def alloc_kv_cache(batch, n_kv_heads, capacity, weight=True, device="cuda"):
+    """An empty cache: lengths and weights 0, K and V uninitialised."""
+    k = torch.empty(batch, n_kv_heads, capacity, 128, dtype=torch.bfloat16, device=device)
+    lens = torch.zeros(batch, dtype=torch.int32, device=device)
+    w = torch.zeros(batch, n_kv_heads, capacity, dtype=torch.float32, device=device) if weight else None
+    return KVCache(k, torch.empty_like(k), lens, w)
+
+
+_WEIGHTS = {None: 0, "set": 1, "add": 2}
+
+
+def _queries(q, o, cache, scale):
+    """q, o: [B, Hq, n_new, 128] ([Hq, n_new, 128] with a cache of one sequence)."""
+    x = _Queries()
+    for t in (q, o):
+        if t is not None:
+            assert t.dtype == torch.bfloat16 and t.stride(-1) == 1, "bf16, head_dim contiguous"
+            assert t.dim() in (3, 4) and t.shape == q.shape and t.device == cache.k.device, "o like q, on the cache's device"
+    assert (q.shape[0] if q.dim() == 4 else 1) == cache.batch and q.shape[-1] == cache.k.shape[-1], "q and cache differ"
+    x.q, x.o = q.data_ptr(), o.data_ptr() if o is not None else None
+    x.q_stride[:] = _strides4(q)[0]
+    x.o_stride[:] = _strides4(o)[0] if o is not None else (0, 0, 0)
+    x.n_q_heads, x.n_new, x.softmax_scale = q.shape[-3], q.shape[-2], float(scale)
+    return x
+
+
+def _cache_call(fn, device, ws, stream, *args):
+    """On the tensors' device, its current stream unless another one is given."""
+    assert ws.device == device, "workspace on the cache's device"
+    with torch.cuda.device(device):
+        _check(fn(*args, ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def minf_cache_attn_workspace_bytes(q, cache, n_init=0, n_local=None, weights=None):
+    x, c = _queries(q, None, cache, 0.0), cache.c_struct()
+    return int(lib().minf_cache_attn_workspace_bytes(ctypes.byref(x), ctypes.byref(c), n_init,
+                                                     cache.capacity if n_local is None else n_local, _WEIGHTS[weights]))
+
+
+def minf_prefix_attn_workspace_bytes(q, prefix, cache):
+    x, p, c = _queries(q, None, cache, 0.0), prefix.c_struct(), cache.c_struct()
+    return int(lib().minf_prefix_attn_workspace_bytes(ctypes.byref(x), ctypes.byref(p), ctypes.byref(c)))
+
+
+def minf_cache_evict_workspace_bytes(cache, keep):
+    c = cache.c_struct()
+    return int(lib().minf_cache_evict_workspace_bytes(ctypes.byref(c), keep))
+
+
+def minf_cache_attn(q, o, cache, ws, n_init=0, n_local=None, weights=None, scale=0.0, stream=None):
+    """o = attention of the newest tokens q against the cache, sink + sliding window (n_local=None: the
+    whole cache); weights="set" / "add": cache.weight receives the attention weight of every slot."""
+    x, c = _queries(q, o, cache, scale), cache.c_struct()
+    _cache_call(lib().minf_cache_attn, cache.k.device, ws, stream, ctypes.byref(x), ctypes.byref(c), n_init,
+                cache.capacity if n_local is None else n_local, _WEIGHTS[weights])
+
+
+def minf_prefix_attn(q, o, prefix, cache, ws, scale=0.0, stream=None):
+    """o = attention of the newest tokens q against a prefix that all sequences share (a cache of one
+    sequence) and, behind it, their own caches."""
+    assert prefix.k.device == cache.k.device, "one device"
+    x, p, c = _queries(q, o, cache, scale), prefix.c_struct(), cache.c_struct()
+    _cache_call(lib().minf_prefix_attn, cache.k.device, ws, stream, ctypes.byref(x), ctypes.byref(p), ctypes.byref(c))
+
+
+def minf_cache_evict(cache, keep, ws, kept, to=None, n_init=0, n_recent=0, stream=None):
+    """Keeps, per sequence and K/V head, `keep` slots: the first n_init, the last n_recent and those of the
+    largest weight; moves them to the front of `to` (None: in place).  kept [B, Hkv, keep] int32."""
+    to = cache if to is None else to
+    batch, heads, _ = cache._args()
+    assert kept.dtype == torch.int32 and kept.is_contiguous() and kept.numel() == batch * heads * keep, \
+        "kept: int32 [B, Hkv, keep]"
+    assert kept.device == cache.k.device and to.k.device == cache.k.device, "one device"
+    c, t = cache.c_struct(), to.c_struct()
+    _cache_call(lib().minf_cache_evict, cache.k.device, ws, stream, ctypes.byref(c), n_init, n_recent, keep,
+                ctypes.byref(t), ctypes.c_void_p(kept.data_ptr()))

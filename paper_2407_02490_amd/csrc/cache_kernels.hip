@@ -1,0 +1,684 @@
+// Attention of new tokens against a KV cache, and eviction from it, for gfx950 (MI355X).
+//
+//   o_i = sum_j p_ij v_j,  p_ij = exp(c q_i k_j - m_i) / sum_j' exp(c q_i k_j' - m_i),  j over the visible slots
+//   w_j (+)= sum over the rows i of a K/V head's group of p_ij
+//
+// Every key costs 512 bytes and, with R rows per K/V head, 512 R flops: with the 4 to 64 rows of a decode step
+// the memory bounds it, so the kernel is built to keep loads in flight.  A wave is a worker of its own: it
+// takes a consecutive share of the tiles of all sequences (cache_walk.h), fetches tile t+1 into its half of an
+// LDS ring (global -> LDS, no registers) while it computes tile t, and meets no barrier.  Rows are the columns
+// of 32x32x16 MFMAs (S^T = K Q^T, O^T += V^T P^T, as in the prefill kernels), so P never leaves registers.
+// A segment (row tile of a sequence and K/V head) that several workers share leaves pieces (maximum, sum,
+// unnormalised O) in the workspace, which cache_join_kernel joins.
+#include "cache_walk.h"
+#include "mfma_tile.h"
+
+namespace minf {
+
+constexpr int CACHE_WAVES = 4;                                  // per workgroup
+constexpr int CACHE_RING = 2 * 2 * HALF_BYTES;                  // per wave: two slots of a K and a V tile
+static_assert(CACHE_TILE * ROW_BYTES == HALF_BYTES, "a tile of the walk is half a 64-key tile");
+
+__device__ inline int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// ---- where a worker is in the list of tiles (wave-uniform) --------------------------------------------
+struct CacheCursor {
+  int prefix;            // 1: the shared prefix
+  int b, kvh, rt;        // sequence, K/V head, row tile
+  int tau;               // tile of the segment
+  SeqWalk w;             // of the sequence (or of the prefix)
+};
+
+__device__ inline SeqWalk walk_of(const CacheCall &x, int b) {
+  return seq_walk(x.lens[b], x.capacity, x.n_new, x.n_init, x.n_local);
+}
+__device__ inline SeqWalk walk_of_uniform(const CacheCall &x, int b) {
+  return seq_walk(uni(x.lens[uni(b)]), x.capacity, x.n_new, x.n_init, x.n_local);
+}
+// The prefix: every row sees all of it.
+__device__ inline SeqWalk prefix_walk(const CacheCall &x) {
+  return seq_walk(x.p_cap > 0 ? uni(x.p_lens[0]) : 0, x.p_cap, 1, 0, x.p_cap);
+}
+
+__device__ inline int wave_scan(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(v, d);
+    if (lane >= d) v += u;
+  }
+  return v;
+}
+
+// Tiles in front of the own segments of sequence b (b = batch: all of them), per K/V head and row tile.
+__device__ inline int tiles_before(const CacheCall &x, int b, int lane) {
+  int sum = 0;
+  for (int b0 = 0; b0 < b; b0 += 64) {
+    const int i = b0 + lane;
+    int t = i < b ? walk_of(x, i).tiles : 0;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) t += __shfl_xor(t, d);
+    sum += t;
+  }
+  return uni(sum);
+}
+
+// Cursor at tile g of the list; pre: tiles of the prefix.
+__device__ inline void seek(const CacheCall &x, int g, int pre, CacheCursor &c, int lane) {
+  if (g < pre) {
+    c.prefix = 1;
+    c.w = prefix_walk(x);
+    const int s = g / c.w.tiles;
+    c.tau = g - s * c.w.tiles;
+    c.b = 0; c.kvh = s / x.p_row_tiles; c.rt = s - c.kvh * x.p_row_tiles;
+    return;
+  }
+  g -= pre;
+  const int heads = x.n_kv * x.row_tiles;
+  int before = 0;
+  c.prefix = 0;
+  for (int b0 = 0; b0 < x.batch; b0 += 64) {
+    const int i = b0 + lane, t = i < x.batch ? walk_of(x, i).tiles : 0;
+    const int incl = wave_scan(t, lane);
+    const unsigned long long beyond = __builtin_amdgcn_ballot_w64((before + incl) * heads > g);
+    if (beyond != 0) {
+      const int at = __builtin_ctzll(beyond);
+      c.b = b0 + at;
+      before += uni(__shfl(incl, at)) - uni(__shfl(t, at));
+      break;
+    }
+    before += uni(__shfl(incl, 63));
+  }
+  c.b = uni(c.b);
+  c.w = walk_of_uniform(x, c.b);
+  g -= before * heads;
+  const int s = g / c.w.tiles;
+  c.tau = uni(g - s * c.w.tiles);
+  c.kvh = uni(s / x.row_tiles);
+  c.rt = uni(s - c.kvh * x.row_tiles);
+}
+
+// To the next tile of the list.  False at its end.
+__device__ inline bool advance(const CacheCall &x, CacheCursor &c) {
+  if (++c.tau < c.w.tiles) return true;
+  c.tau = 0;
+  if (++c.rt < (c.prefix ? x.p_row_tiles : x.row_tiles)) return true;
+  c.rt = 0;
+  if (++c.kvh < x.n_kv) return true;
+  c.kvh = 0;
+  if (c.prefix) { c.prefix = 0; c.b = -1; }
+  for (;;) {
+    if (++c.b >= x.batch) return false;
+    c.w = walk_of_uniform(x, c.b);
+    if (c.w.tiles > 0) return true;
+  }
+}
+
+__device__ inline int segment_of(const CacheCall &x, const CacheCursor &c) {
+  return c.prefix ? c.kvh * x.p_row_tiles + c.rt
+                  : x.n_kv * x.p_row_tiles + (c.b * x.n_kv + c.kvh) * x.row_tiles + c.rt;
+}
+
+// ---- tile arithmetic ------------------------------------------------------------------------------------
+// Rows of a segment: 32 NT per row tile.  Row r of a sequence is token r / group of the n_new, query head
+// r % group of the K/V head's group; rows of the prefix are those of all sequences, one after the other.
+template <int NT>
+struct CacheRows {
+  bf16x8 q[NT][8];
+  f32x16 o[NT][4];        // [row half][d block]
+  float m[NT], l[NT];     // running maximum (base 2), this lane's share of the running sum
+  int pos[NT];            // position of this lane's row: it sees the slots up to there
+  int tok[NT];            // its token, 0 .. n_new - 1
+};
+
+struct LaneRow {
+  int b, t, g;
+};
+__device__ inline LaneRow lane_row(const CacheCall &x, const CacheCursor &c, int row) {
+  LaneRow a;
+  a.b = c.b;
+  int r = row;
+  if (c.prefix) { a.b = r / x.rows; r -= a.b * x.rows; }
+  a.t = r / x.group;
+  a.g = r - a.t * x.group;
+  return a;
+}
+
+template <int NT>
+__device__ inline void begin_segment(const CacheCall &x, const CacheCursor &c, CacheRows<NT> &st, int lane) {
+  const int n = lane & 31, h = lane >> 5, last = (c.prefix ? x.batch * x.rows : x.rows) - 1;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    // rows behind the last one repeat it; nobody stores them
+    const LaneRow a = lane_row(x, c, min((c.rt * NT + nt) * 32 + n, last));
+    const bf16_t *row = x.q + a.b * x.q_sb + (int64_t)(c.kvh * x.group + a.g) * x.q_sh + a.t * x.q_st + 8 * h;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) st.q[nt][ks] = *reinterpret_cast<const bf16x8 *>(row + 16 * ks);
+    st.tok[nt] = c.prefix ? 0 : a.t;
+    st.pos[nt] = c.prefix ? c.w.len - 1 : c.w.i0 + a.t;
+    st.m[nt] = -INFINITY;
+    st.l[nt] = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[nt][db][r] = 0.f;
+  }
+}
+
+__device__ inline bool tile_not_finite(const char *tV, int lane) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < HALF_BYTES / 1024; ++i) {
+    const uint4 w = *reinterpret_cast<const uint4 *>(tV + i * 1024 + lane * 16);
+    const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      bad = bad || (u[j] & 0x7f80u) == 0x7f80u || (u[j] & 0x7f800000u) == 0x7f800000u;
+  }
+  return __builtin_amdgcn_ballot_w64(bad) != 0;
+}
+
+// O^T += V^T P^T for the tokens one by one, with the V rows that a token does not see as zeros: 0 * inf and
+// 0 * NaN of a slot that a row's mask excludes would otherwise reach the row.  Only tiles with a mask and
+// with such values take it.
+template <int NT>
+__device__ inline void update_by_token(CacheRows<NT> &st, const bf16x8 (&p)[NT][2][2],
+                                                          const char *tV, int kb, int n_tok, int first_pos,
+                                                          int n_init, int n_local, int lane) {
+  LaneOfs lo;
+  lane_offsets(lo, lane);
+  const int h = lane >> 5;
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int t = 0; t < n_tok; ++t) {
+    unsigned sees[2] = {0u, 0u};
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (cache_visible(kb + 16 * tt + 8 * h + e, first_pos + t, n_init, n_local)) sees[tt] |= 1u << e;
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      bf16x8 a[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        s16x8 w = __builtin_bit_cast(s16x8, lds_read_vt(tV, lo.v[db][0] + 16 * tt * ROW_BYTES,
+                                                        lo.v[db][1] + 16 * tt * ROW_BYTES));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (sees[tt] >> e) & 1 ? w[e] : (short)0;
+        a[tt] = __builtin_bit_cast(bf16x8, w);
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        f32x16 add = zero;
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+            add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[tt], p[nt][tt][part], add, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st.o[nt][db][r] += st.tok[nt] == t ? add[r] : 0.f;
+      }
+    }
+  }
+}
+
+// One tile of 32 keys from slot kb on.  Register r of s holds key 16 (r / 8) + 8 h + r % 8 of row n.
+template <int NT>
+__device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, CacheRows<NT> &st, const LaneOfs &lo,
+                                  const char *tK, const char *tV, int lane) {
+  const int n = lane & 31, h = lane >> 5, kb = c.w.base(c.tau);
+  f32x16 s[NT];
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) {
+    const bf16x8 a = lds_read_k(tK, lo.k[ks]);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      s[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, st.q[nt][ks], ks == 0 ? zero : s[nt], 0, 0, 0);
+    }
+  }
+  const int n_init = c.prefix ? 0 : x.n_init, n_local = c.prefix ? x.p_cap : x.n_local;
+  const int first_pos = c.prefix ? c.w.len - 1 : c.w.i0, last_pos = c.w.len - 1, klast = kb + CACHE_TILE - 1;
+  const bool whole = klast <= first_pos && (klast < n_init || last_pos - kb < n_local);
+  if (!whole) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = kb + 16 * (r >> 3) + 8 * h + (r & 7);
+        s[nt][r] = cache_visible(key, st.pos[nt], n_init, n_local) ? s[nt][r] : -INFINITY;
+      }
+  }
+  if (x.logits && !c.prefix) {
+    float *row0 = x.logits + (((int64_t)c.b * x.n_kv + c.kvh) * x.max_tiles + c.tau) * (x.rows * CACHE_TILE);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = (c.rt * NT + nt) * 32 + n;
+      if (row < x.rows) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 w = {s[nt][4 * i] * x.c_log2, s[nt][4 * i + 1] * x.c_log2, s[nt][4 * i + 2] * x.c_log2,
+                            s[nt][4 * i + 3] * x.c_log2};
+          *reinterpret_cast<float4 *>(row0 + row * CACHE_TILE + 16 * (i >> 1) + 8 * h + 4 * (i & 1)) = w;
+        }
+      }
+    }
+  }
+  // running maximum; the sums and O follow only where a row's maximum grew
+  float m_new[NT];
+  bool grew = false;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float mx = s[nt][0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[nt][r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * x.c_log2;
+    m_new[nt] = fmaxf(st.m[nt], mx);
+    grew = grew || m_new[nt] > st.m[nt];
+  }
+  if (__builtin_amdgcn_ballot_w64(grew) != 0) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float f = m_new[nt] == -INFINITY ? 1.f : fast_exp2(st.m[nt] - m_new[nt]);
+      st.m[nt] = m_new[nt];
+      st.l[nt] *= f;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st.o[nt][db][r] *= f;
+    }
+  }
+  // P as the sum of two bf16 (16 bits of mantissa): the matrix cores idle here, and the output is then as
+  // good as from fp32 weights
+  bf16x8 p[NT][2][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const float m = st.m[nt] == -INFINITY ? 0.f : st.m[nt];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = fast_exp2(fmaf(s[nt][8 * tt + e], x.c_log2, -m));
+        st.l[nt] += v;
+        const __bf16 hi = (__bf16)v;
+        p[nt][tt][0][e] = hi;
+        p[nt][tt][1][e] = (__bf16)(v - (float)hi);
+      }
+  }
+  if (!whole && tile_not_finite(tV, lane)) {
+    update_by_token<NT>(st, p, tV, kb, c.prefix ? 1 : x.n_new, first_pos, n_init, n_local, lane);
+    return;
+  }
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      const bf16x8 a = lds_read_vt(tV, lo.v[db][0] + 16 * tt * ROW_BYTES, lo.v[db][1] + 16 * tt * ROW_BYTES);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+          st.o[nt][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[nt][tt][part], st.o[nt][db], 0, 0, 0);
+    }
+}
+
+// End of a worker's part of a segment: rows of O that are final go out, others into the workspace.
+template <int NT>
+__device__ inline void end_segment(const CacheCall &x, const CacheCursor &c, const CacheRows<NT> &st, bool whole,
+                                   int slot, int lane) {
+  const int n = lane & 31, h = lane >> 5, rows = c.prefix ? x.batch * x.rows : x.rows;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = (c.rt * NT + nt) * 32 + n;
+    const float l = st.l[nt] + __shfl_xor(st.l[nt], 32);
+    if (row >= rows) continue;
+    if (whole && x.p_cap == 0) {
+      const LaneRow a = lane_row(x, c, row);
+      const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+      bf16_t *to = x.o + a.b * x.o_sb + (int64_t)(c.kvh * x.group + a.g) * x.o_sh + a.t * x.o_st + 4 * h;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x2 u = {st.o[nt][db][4 * g] * inv, st.o[nt][db][4 * g + 1] * inv};
+          const f32x2 w = {st.o[nt][db][4 * g + 2] * inv, st.o[nt][db][4 * g + 3] * inv};
+          uint2 two;
+          two.x = __builtin_bit_cast(unsigned, __builtin_convertvector(u, bf16x2));
+          two.y = __builtin_bit_cast(unsigned, __builtin_convertvector(w, bf16x2));
+          *reinterpret_cast<uint2 *>(to + 32 * db + 8 * g) = two;
+        }
+      if (x.stat && h == 0) x.stat[((int64_t)c.b * x.n_kv + c.kvh) * x.rows + row] = float2{st.m[nt], inv};
+      continue;
+    }
+    const int64_t at = (int64_t)slot * x.slot_rows + nt * 32 + n;
+    if (h == 0) x.piece_ml[at] = float2{st.m[nt], l};
+    float *to = x.piece_o + at * D + 4 * h;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 w = {st.o[nt][db][4 * g], st.o[nt][db][4 * g + 1], st.o[nt][db][4 * g + 2], st.o[nt][db][4 * g + 3]};
+        *reinterpret_cast<float4 *>(to + 32 * db + 8 * g) = w;
+      }
+  }
+}
+
+template <int NT>
+__global__ __launch_bounds__(64 * CACHE_WAVES) void cache_attn_kernel(CacheCall x) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
+  const int worker = blockIdx.x * CACHE_WAVES + wave;
+  char *ring = lds + wave * CACHE_RING;
+
+  const int pre = prefix_walk(x).tiles * x.n_kv * x.p_row_tiles;
+  const int total = pre + tiles_before(x, x.batch, lane) * x.n_kv * x.row_tiles;
+  const int share = worker_share(total, x.workers, x.min_tiles);
+  const int g0 = worker * share, g1 = min(g0 + share, total);
+  if (g0 >= g1) return;
+
+  CacheCursor cur, nxt;
+  seek(x, g0, pre, cur, lane);
+  LaneOfs lo;
+  lane_offsets(lo, lane);
+  auto fetch = [&](const CacheCursor &c, int slot) {
+    DmaLane dl;
+    const int kb = c.w.base(c.tau);
+    char *tK = ring + slot * 2 * HALF_BYTES;
+    const int64_t k_st = c.prefix ? x.pk_st : x.k_st, v_st = c.prefix ? x.pv_st : x.v_st;
+    const bf16_t *kh = c.prefix ? x.pk + c.kvh * x.pk_sh : x.k + c.b * x.k_sb + c.kvh * x.k_sh;
+    const bf16_t *vh = c.prefix ? x.pv + c.kvh * x.pv_sh : x.v + c.b * x.v_sb + c.kvh * x.v_sh;
+    dma_lane_init(dl, k_st, lane);
+    dma_rows<1, 32, true>(kh, k_st, dl, kb, nullptr, c.w.len, tK, 0, lane);
+    dma_lane_init(dl, v_st, lane);
+    dma_rows<1, 32, true>(vh, v_st, dl, kb, nullptr, c.w.len, tK + HALF_BYTES, 0, lane);
+  };
+  CacheRows<NT> st;
+  fetch(cur, 0);
+  int piece_t0 = cur.tau;                    // first tile of this worker's part of the segment
+  begin_segment<NT>(x, cur, st, lane);
+  for (int g = g0, slot = 0;; ++g, slot ^= 1) {
+    nxt = cur;
+    const bool more = g + 1 < g1 && advance(x, nxt);
+    if (more) {
+      fetch(nxt, slot ^ 1);
+      MINF_WAIT_VMCNT(16);                   // the 16 loads just issued may still run, the tile's own have landed
+    } else {
+      MINF_WAIT_VMCNT(0);
+    }
+    const char *tK = ring + slot * 2 * HALF_BYTES;
+    cache_tile<NT>(x, cur, st, lo, tK, tK + HALF_BYTES, lane);
+    __builtin_amdgcn_s_waitcnt(0xC07F);      // LDS reads done: the slot may be filled again
+    const bool done = !more || nxt.tau == 0;
+    if (done) {
+      const bool whole = piece_t0 == 0 && cur.tau == cur.w.tiles - 1;
+      const int first_g = g - (cur.tau - piece_t0);
+      end_segment<NT>(x, cur, st, whole, whole ? 2 * x.workers + segment_of(x, cur) : 2 * worker + (first_g > g0 ? 1 : 0), lane);
+      if (!more) break;
+      begin_segment<NT>(x, nxt, st, lane);
+      piece_t0 = 0;
+    }
+    cur = nxt;
+  }
+}
+
+// ---- joining the pieces ---------------------------------------------------------------------------------
+// One workgroup per output row: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the pieces of the row's
+// own segment and of the prefix's.  Rows without a visible key, or without a token, give zeros.
+constexpr int JOIN_WAVES = 4;
+__global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x, int tile_rows) {
+  const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
+  const int row = blockIdx.x % x.rows, seg = blockIdx.x / x.rows;      // of the sequence and K/V head
+  const int b = seg / x.n_kv, kvh = seg - b * x.n_kv;
+  const int pt = prefix_walk(x).tiles, pre = pt * x.n_kv * x.p_row_tiles;
+  const int heads = x.n_kv * x.row_tiles;
+  const int before = tiles_before(x, b, lane);
+  const int total = pre + tiles_before(x, x.batch, lane) * heads;
+  const int share = worker_share(total, x.workers, x.min_tiles);
+  const SeqWalk w = walk_of_uniform(x, b);
+  const int t = row / x.group, rt = row / tile_rows;
+  const bool token = w.i0 + t >= 0;
+  const int own0 = pre + before * heads + (kvh * x.row_tiles + rt) * w.tiles;
+  if (x.p_cap == 0 && w.tiles > 0) {
+    const SegmentPieces p = segment_pieces(own0, own0 + w.tiles, share);
+    if (p.first == p.last) return;                                     // written by the worker itself
+  }
+  float m = -INFINITY, l = 0.f;
+  f32x2 o = {0.f, 0.f};
+  auto add = [&](int64_t at) {
+    const float2 ml = x.piece_ml[at];
+    const f32x2 po = *reinterpret_cast<const f32x2 *>(x.piece_o + at * D + 2 * lane);
+    if (ml.x == -INFINITY && ml.y == 0.f) return;                      // no visible key in the piece
+    const float mn = fmaxf(m, ml.x);
+    const float f = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - mn), g = fast_exp2(ml.x - mn);
+    m = mn;
+    l = l * f + ml.y * g;
+    o[0] = o[0] * f + po[0] * g;
+    o[1] = o[1] * f + po[1] * g;
+  };
+  auto join = [&](int t0, int tiles, int in_tile, int segment) {
+    if (tiles <= 0) return;
+    const SegmentPieces p = segment_pieces(t0, t0 + tiles, share);
+    if (p.first == p.last) {
+      if (wave == 0) add((int64_t)(2 * x.workers + segment) * x.slot_rows + in_tile);
+      return;
+    }
+    for (int i = p.first + wave; i <= p.last; i += JOIN_WAVES)
+      add((int64_t)piece_slot(i, t0, share) * x.slot_rows + in_tile);
+  };
+  if (token) {
+    join(own0, w.tiles, row - rt * tile_rows, x.n_kv * x.p_row_tiles + (b * x.n_kv + kvh) * x.row_tiles + rt);
+    if (x.p_cap > 0) {
+      const int prow = b * x.rows + row, prt = prow / tile_rows;
+      join((kvh * x.p_row_tiles + prt) * pt, pt, prow - prt * tile_rows, kvh * x.p_row_tiles + prt);
+    }
+  }
+  __shared__ float sm[JOIN_WAVES], sl[JOIN_WAVES];
+  __shared__ f32x2 so[JOIN_WAVES][64];
+  if (lane == 0) { sm[wave] = m; sl[wave] = l; }
+  so[wave][lane] = o;
+  __syncthreads();
+  if (wave != 0) return;
+  m = -INFINITY; l = 0.f;
+  o = f32x2{0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < JOIN_WAVES; ++i) m = fmaxf(m, sm[i]);
+#pragma unroll
+  for (int i = 0; i < JOIN_WAVES; ++i) {
+    if (sm[i] == -INFINITY && sl[i] == 0.f) continue;
+    const float f = fast_exp2(sm[i] - m);
+    l += sl[i] * f;
+    o[0] += so[i][lane][0] * f;
+    o[1] += so[i][lane][1] * f;
+  }
+  const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+  const f32x2 r = {o[0] * inv, o[1] * inv};
+  bf16_t *to = x.o + b * x.o_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.o_sh + t * x.o_st;
+  *reinterpret_cast<unsigned *>(to + 2 * lane) = __builtin_bit_cast(unsigned, __builtin_convertvector(r, bf16x2));
+  if (x.stat && lane == 0) x.stat[(int64_t)seg * x.rows + row] = float2{m, inv};
+}
+
+// Weight of every slot: the column sums of the softmax, from the logits that the workers left.
+__global__ __launch_bounds__(256) void cache_weight_kernel(CacheCall x) {
+  const int slot = blockIdx.x * 256 + threadIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+  const SeqWalk w = walk_of(x, b);
+  if (slot >= w.len) return;
+  const int tau = w.tile_of(slot);
+  float sum = 0.f;
+  if (tau >= 0) {
+    const int64_t head = (int64_t)b * x.n_kv + kvh;
+    const float *s = x.logits + (head * x.max_tiles + tau) * (x.rows * CACHE_TILE) + (slot - w.base(tau));
+    const float2 *st = x.stat + head * x.rows;
+    for (int r = 0; r < x.rows; ++r) {
+      const float v = s[r * CACHE_TILE];
+      const float2 ml = st[r];
+      sum += v == -INFINITY ? 0.f : fast_exp2(v - ml.x) * ml.y;
+    }
+  }
+  float *to = x.weight + b * x.w_sb + kvh * x.w_sh + slot;
+  *to = x.add_weights ? *to + sum : sum;
+}
+
+// ---- eviction ---------------------------------------------------------------------------------------------
+// Order of the weights as unsigned numbers: NaN lowest, -0 and 0 equal.
+__device__ inline unsigned weight_key(float v) {
+  if (v != v) return 0u;
+  const unsigned u = v == 0.f ? 0u : __builtin_bit_cast(unsigned, v);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+constexpr int SELECT_THREADS = 1024;
+// Sum of v over the lower threads of the workgroup, and over all of them.  part: SELECT_THREADS / 64 + 1 words.
+__device__ inline int block_scan(int v, int *part, int &all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockDim.x >> 6;
+  const int incl = wave_scan(v, lane);
+  __syncthreads();
+  if (lane == 63) part[wave] = incl;
+  __syncthreads();
+  int before = 0;
+  all = 0;
+  for (int i = 0; i < n; ++i) {
+    if (i < wave) before += part[i];
+    all += part[i];
+  }
+  return before + incl - v;
+}
+
+// Kept slots of one sequence and K/V head: the keep largest weights in four passes over eight bits each, from
+// the most significant one; then the slots in ascending order.
+__global__ __launch_bounds__(SELECT_THREADS) void cache_select_kernel(EvictCall x) {
+  __shared__ int hist[256], part[SELECT_THREADS / 64], pick[2];
+  const int row = blockIdx.x, b = row / x.n_kv, kvh = row - b * x.n_kv, tid = threadIdx.x;
+  const int len = min(max(x.lens[b], 0), x.capacity), n = min(len, x.keep);
+  int32_t *kept = x.kept + (int64_t)row * x.keep;
+  if (tid == 0) x.counts[row] = n;
+  if (len <= x.keep) {
+    for (int i = tid; i < x.keep; i += SELECT_THREADS) kept[i] = i < len ? i : -1;
+    return;
+  }
+  const float *w = x.weight + b * x.w_sb + kvh * x.w_sh;
+  const int first = x.n_init, last = len - x.n_recent;
+  int want = x.keep - x.n_init - x.n_recent;             // of the slots first .. last - 1
+  unsigned prefix = 0, mask = 0;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += SELECT_THREADS) hist[i] = 0;
+    __syncthreads();
+    for (int i = first + tid; i < last; i += SELECT_THREADS) {
+      const unsigned k = weight_key(w[i]);
+      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int above = 0, d = 255;
+      while (d > 0 && above + hist[d] < want) above += hist[d--];
+      pick[0] = d;
+      pick[1] = above;
+    }
+    __syncthreads();
+    prefix |= (unsigned)pick[0] << shift;
+    mask |= 255u << shift;
+    want -= pick[1];
+    __syncthreads();
+  }
+  // `want` of the slots whose weight equals the last kept one, the lowest ones
+  int out = 0, equal_before = 0;
+  for (int i0 = 0; i0 < len; i0 += SELECT_THREADS) {
+    const int i = i0 + tid;
+    const bool forced = i < first || (i >= last && i < len);
+    const unsigned k = i >= first && i < last ? weight_key(w[i]) : 0u;
+    const bool middle = i >= first && i < last;
+    const bool equal = middle && k == prefix;
+    int equals, takes;
+    const int e = block_scan(equal ? 1 : 0, part, equals);
+    const bool take = forced || (middle && k > prefix) || (equal && equal_before + e < want);
+    const int at = block_scan(take ? 1 : 0, part, takes);
+    if (take) kept[out + at] = i;
+    out += takes;
+    equal_before += equals;
+  }
+}
+
+// Moves the kept rows to the slots 0, 1, ...  A workgroup owns one slice of 64 bytes of the rows of K or V of
+// one sequence and K/V head (slices 0..3: K, 4..7: V), or its weights (slice 8), and walks them in ascending
+// order, a chunk into registers, then out.  In place that is safe: the kept slots ascend, so the rows of a
+// later chunk lie behind everything that this chunk overwrites.
+constexpr int MOVE_SLICES = 9, MOVE_ROWS = 256;
+__global__ __launch_bounds__(256) void cache_move_kernel(EvictCall x, int in_place) {
+  const int slice = blockIdx.x, row = blockIdx.y, b = row / x.n_kv, kvh = row - b * x.n_kv, tid = threadIdx.x;
+  const int n = x.counts[row];
+  const int32_t *kept = x.kept + (int64_t)row * x.keep;
+  const int step = in_place ? MOVE_ROWS : MOVE_ROWS * gridDim.z;
+  if (slice == 8) {
+    const float *from = x.weight + b * x.w_sb + kvh * x.w_sh;
+    float *to = x.to_weight + b * x.tw_sb + kvh * x.tw_sh;
+    for (int i0 = blockIdx.z * MOVE_ROWS; i0 < n; i0 += step) {
+      const int i = i0 + tid;
+      float v = 0.f;
+      if (i < n) v = from[kept[i]];
+      asm volatile("" : "+v"(v));
+      __syncthreads();
+      if (i < n) to[i] = v;
+    }
+    // in place: behind the reads of all kept weights
+    __syncthreads();
+    for (int i = n + (int)blockIdx.z * MOVE_ROWS + tid; i < x.to_capacity; i += MOVE_ROWS * gridDim.z) to[i] = 0.f;
+    if (kvh == 0 && blockIdx.z == 0 && tid == 0) x.to_lens[b] = n;
+    return;
+  }
+  const bool is_v = slice >= 4;
+  const int64_t f_st = is_v ? x.v_st : x.k_st, t_st = is_v ? x.tv_st : x.tk_st;
+  const bf16_t *from = (is_v ? x.v + b * x.v_sb + kvh * x.v_sh : x.k + b * x.k_sb + kvh * x.k_sh) + 32 * (slice & 3) + 8 * (tid & 3);
+  bf16_t *to = (is_v ? x.to_v + b * x.tv_sb + kvh * x.tv_sh : x.to_k + b * x.tk_sb + kvh * x.tk_sh) + 32 * (slice & 3) + 8 * (tid & 3);
+  for (int i0 = blockIdx.z * MOVE_ROWS; i0 < n; i0 += step) {
+    const int end = min(i0 + MOVE_ROWS, n);
+    if (in_place && kept[end - 1] == end - 1) continue;          // nothing evicted in front of these rows
+    uint4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + 64 * j + (tid >> 2);
+      v[j] = uint4{0u, 0u, 0u, 0u};
+      if (i < end) v[j] = *reinterpret_cast<const uint4 *>(from + kept[i] * f_st);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
+    __syncthreads();                                             // every row of the chunk has been read
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + 64 * j + (tid >> 2);
+      if (i < end) *reinterpret_cast<uint4 *>(to + i * t_st) = v[j];
+    }
+  }
+}
+
+// ---- host-side launches -------------------------------------------------------------------------------------
+template <int NT>
+static hipError_t launch_workers(const CacheCall &x, hipStream_t st) {
+  const size_t lds = CACHE_WAVES * CACHE_RING;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_attn_kernel<NT>),
+                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(cache_attn_kernel<NT>, dim3(x.workers / CACHE_WAVES), dim3(64 * CACHE_WAVES), lds, st, x);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
+  hipError_t e = x.wide ? launch_workers<2>(x, st) : launch_workers<1>(x, st);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(cache_join_kernel, dim3(x.batch * x.n_kv * x.rows), dim3(64 * JOIN_WAVES), 0, st, x,
+                     x.wide ? 64 : 32);
+  if ((e = hipGetLastError()) != hipSuccess || !x.weight) return e;
+  hipLaunchKernelGGL(cache_weight_kernel, dim3((x.capacity + 255) / 256, x.n_kv, x.batch), dim3(256), 0, st, x);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_evict(const EvictCall &x, bool in_place, hipStream_t st) {
+  const int rows = x.batch * x.n_kv;
+  hipLaunchKernelGGL(cache_select_kernel, dim3(rows), dim3(SELECT_THREADS), 0, st, x);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int chunks = (x.keep + MOVE_ROWS - 1) / MOVE_ROWS;
+  hipLaunchKernelGGL(cache_move_kernel, dim3(MOVE_SLICES, rows, in_place ? 1 : (chunks < 1024 ? chunks : 1024)), dim3(256), 0,
+                     st, x, in_place ? 1 : 0);
+  return hipGetLastError();
+}
+
+}  // namespace minf

@@ -1,0 +1,75 @@
+// How the cache calls cut their work (plain C++: the kernels use it, and a test enumerates it on the host).
+//
+// A sequence's keys are walked in tiles of 32: of the slots 0 .. len-1 those that some of its n_new rows
+// can see, the first n_init ones and the window that ends at the last token.  The tiles of all sequences and
+// K/V heads form one list, and every worker (a wave) takes an equal, consecutive share of it: a batch of
+// unequal lengths fills the chip as evenly as one of equal ones, and the lengths stay on the device.
+#ifndef MINF_CACHE_WALK_H_
+#define MINF_CACHE_WALK_H_
+
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define MINF_HD __host__ __device__ inline
+#else
+#define MINF_HD inline
+#endif
+
+namespace minf {
+
+constexpr int CACHE_TILE = 32;
+
+// Tiles of one sequence: T1 tiles of the sink from slot 0 on, then the window's from slot s2 (a multiple of
+// the tile) on.  Sink and window that touch in a tile are walked as one (T1 = 0, s2 = 0).
+struct SeqWalk {
+  int32_t len, i0, T1, s2, tiles;       // i0: position of the first of the n_new rows (negative: no token)
+  MINF_HD int32_t base(int32_t t) const { return t < T1 ? t * CACHE_TILE : s2 + (t - T1) * CACHE_TILE; }
+  // tile that holds a slot, or -1
+  MINF_HD int32_t tile_of(int32_t slot) const {
+    if (slot < T1 * CACHE_TILE) return slot / CACHE_TILE;
+    return slot >= s2 && slot < len ? T1 + (slot - s2) / CACHE_TILE : -1;
+  }
+};
+
+// n_init, n_local: at most the capacity, so that no sum here leaves 32 bits.
+MINF_HD SeqWalk seq_walk(int32_t len, int32_t capacity, int32_t n_new, int32_t n_init, int32_t n_local) {
+  SeqWalk w;
+  w.len = len < 0 ? 0 : (len > capacity ? capacity : len);
+  w.i0 = w.len - n_new;
+  const int32_t e1 = n_init < w.len ? n_init : w.len;
+  const int32_t lo = w.i0 - n_local + 1;
+  w.s2 = lo > 0 ? lo / CACHE_TILE * CACHE_TILE : 0;
+  w.T1 = (e1 + CACHE_TILE - 1) / CACHE_TILE;
+  if (w.s2 <= w.T1 * CACHE_TILE) w.s2 = w.T1 = 0;
+  w.tiles = w.T1 + (w.len - w.s2 + CACHE_TILE - 1) / CACHE_TILE;
+  return w;
+}
+
+MINF_HD bool cache_visible(int32_t key, int32_t pos, int32_t n_init, int32_t n_local) {
+  return key <= pos && (key < n_init || pos - key < n_local);
+}
+
+// Tiles per worker: equal shares, but at least min_tiles.
+MINF_HD int32_t worker_share(int32_t total, int32_t workers, int32_t min_tiles) {
+  const int32_t c = (total + workers - 1) / workers;
+  return c < min_tiles ? min_tiles : c;
+}
+
+// Workers of the segment (one row tile of one sequence and K/V head) that holds the tiles [t0, t1) of the
+// list: first .. last.  The part that begins at a worker's own first tile is its piece 0, another one its
+// piece 1: no worker has more than two parts of segments that it does not hold whole.
+struct SegmentPieces {
+  int32_t first, last;
+};
+MINF_HD SegmentPieces segment_pieces(int32_t t0, int32_t t1, int32_t share) {
+  SegmentPieces p;
+  p.first = t0 / share;
+  p.last = (t1 - 1) / share;
+  return p;
+}
+MINF_HD int32_t piece_slot(int32_t worker, int32_t t0, int32_t share) {
+  return 2 * worker + (t0 > worker * share ? 1 : 0);
+}
+
+}  // namespace minf
+#endif

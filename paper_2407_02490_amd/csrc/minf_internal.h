@@ -219,5 +219,39 @@ hipError_t launch_vs_lines(int N, int rows, int nv, int ns, const int32_t *s_idx
 hipError_t launch_build_bs(const QKV &x, int nb, const HeadList &hl, int topk, int32_t *blk_idx,
                            int32_t *blk_cnt, int32_t *order, void *ws, hipStream_t st);
 
+// ---- the cache calls (cache_kernels.hip) --------------------------------------------------------------------
+// Pointers of device memory, strides in elements (_sb: sequence, _sh: head, _st: token).
+struct CacheCall {
+  const bf16_t *q, *k, *v, *pk, *pv;    // pk, pv: the shared prefix, or NULL
+  bf16_t *o;
+  const int32_t *lens, *p_lens;
+  float *weight;                        // NULL: no weights
+  int64_t q_sb, q_sh, q_st, o_sb, o_sh, o_st, k_sb, k_sh, k_st, v_sb, v_sh, v_st;
+  int64_t pk_sh, pk_st, pv_sh, pv_st, w_sb, w_sh;
+  int32_t batch, n_kv, group, n_new, capacity, n_init, n_local, add_weights;
+  int32_t rows, row_tiles;              // rows of a K/V head (group * n_new), in tiles of 32 or (wide) 64
+  int32_t p_cap, p_row_tiles;           // capacity of the prefix (0: none), row tiles of its batch * rows rows
+  int32_t wide, workers, min_tiles, max_tiles, slot_rows;
+  float c_log2;
+  // workspace
+  float *logits;                        // [sequence, K/V head, max_tiles][rows][32], base 2; NULL: no weights
+  float2 *stat;                         // [sequence, K/V head, rows]: maximum, 1 / sum; NULL: no weights
+  float2 *piece_ml;                     // [2 workers + segments][slot_rows]: maximum, sum
+  float *piece_o;                       // [2 workers + segments][slot_rows][128]
+};
+hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st);
+
+struct EvictCall {
+  const bf16_t *k, *v;
+  bf16_t *to_k, *to_v;
+  const float *weight;
+  float *to_weight;
+  const int32_t *lens;
+  int32_t *to_lens, *kept, *counts;     // counts (workspace) [sequence, K/V head]: kept slots
+  int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st, w_sb, w_sh, tk_sb, tk_sh, tk_st, tv_sb, tv_sh, tv_st, tw_sb, tw_sh;
+  int32_t batch, n_kv, capacity, to_capacity, n_init, n_recent, keep;
+};
+hipError_t launch_cache_evict(const EvictCall &x, bool in_place, hipStream_t st);
+
 }  // namespace minf
 #endif

@@ -1,0 +1,95 @@
+// Host check of csrc/cache_walk.h: every slot that some row sees lies in exactly one tile of the walk, no tile
+// starts behind the length, max_tiles' bound holds, and the workers' shares cut the list of all segments into
+// pieces whose slots are distinct.
+#include <cstdio>
+#include <set>
+#include <vector>
+
+#include "cache_walk.h"
+
+using namespace minf;
+
+static int fails = 0;
+#define CHECK(c)                                                 \
+  if (!(c)) {                                                    \
+    if (fails++ < 10) printf("FAIL line %d: %s\n", __LINE__, #c); \
+  }
+
+static int walks() {
+  int cases = 0;
+  const int caps[] = {1, 31, 32, 33, 64, 100, 257, 500};
+  const int news[] = {1, 2, 5, 33, 64};
+  const int inits[] = {0, 1, 31, 32, 40, 200, 500};
+  const int locals[] = {1, 2, 31, 32, 33, 64, 100, 500};
+  for (int cap : caps)
+    for (int T : news)
+      for (int ni : inits)
+        for (int nl : locals) {
+          if (ni > cap || nl > cap) continue;
+          const int bound_keys = ni + nl + T + 2 * CACHE_TILE;
+          const int bound = ((bound_keys < cap ? bound_keys : cap) + CACHE_TILE - 1) / CACHE_TILE;
+          for (int len = -1; len <= cap + 1; len += (cap > 100 ? 7 : 1)) {
+            const SeqWalk w = seq_walk(len, cap, T, ni, nl);
+            ++cases;
+            CHECK(w.len == (len < 0 ? 0 : len > cap ? cap : len));
+            CHECK(w.tiles >= 0 && w.tiles <= bound);
+            std::vector<int> times(cap + CACHE_TILE, 0);
+            for (int t = 0; t < w.tiles; ++t) {
+              CHECK(w.base(t) >= 0 && w.base(t) < w.len && w.base(t) % CACHE_TILE == 0);
+              for (int i = 0; i < CACHE_TILE; ++i) {
+                ++times[w.base(t) + i];
+                if (w.base(t) + i < w.len) CHECK(w.tile_of(w.base(t) + i) == t);
+              }
+            }
+            for (int j = 0; j < w.len; ++j) {
+              bool seen = false;
+              for (int t = 0; t < T; ++t) seen = seen || (w.i0 + t >= 0 && cache_visible(j, w.i0 + t, ni, nl));
+              CHECK(times[j] <= 1);
+              CHECK(!seen || times[j] == 1);
+              CHECK((w.tile_of(j) >= 0) == (times[j] == 1));
+            }
+          }
+        }
+  return cases;
+}
+
+static int shares() {
+  int cases = 0;
+  const std::vector<std::vector<int>> lists = {{1}, {5, 0, 3}, {40, 1, 1, 1, 300, 2}, {0, 0}, {7, 7, 7, 7, 7, 7, 7}, {5000}};
+  for (const auto &tiles : lists)
+    for (int workers : {1, 4, 64, 1024})
+      for (int least : {1, 2, 8}) {
+        ++cases;
+        int total = 0;
+        for (int t : tiles) total += t;
+        const int share = worker_share(total, workers, least);
+        CHECK((int64_t)share * workers >= total);
+        std::set<int> used;
+        int t0 = 0;
+        for (int t : tiles) {
+          if (t == 0) continue;
+          const SegmentPieces p = segment_pieces(t0, t0 + t, share);
+          CHECK(p.first >= 0 && p.last < workers && p.first <= p.last);
+          if (p.first != p.last) {
+            int covered = 0;
+            for (int w = p.first; w <= p.last; ++w) {
+              const int a = t0 > w * share ? t0 : w * share, b = t0 + t < (w + 1) * share ? t0 + t : (w + 1) * share;
+              CHECK(b > a);
+              covered += b - a;
+              const int slot = piece_slot(w, t0, share);
+              CHECK(slot == 2 * w + (a > w * share));      // as the worker numbers it
+              CHECK(used.insert(slot).second);
+            }
+            CHECK(covered == t);
+          }
+          t0 += t;
+        }
+      }
+  return cases;
+}
+
+int main() {
+  const int a = walks(), b = shares();
+  if (fails == 0) printf("ok walks %d shares %d\n", a, b);
+  return fails != 0;
+}
