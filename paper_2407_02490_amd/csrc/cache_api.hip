@@ -182,6 +182,28 @@ minf_status run_plan(const minf_queries *q, const minf_kv_cache *c, const minf_k
   return launch_cache_attn(p.x, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? MINF_OK : MINF_ERR_HIP;
 }
 
+// The selection's cut and workspace.  Rows of up to 16K slots: one workgroup per row.  Longer ones in chunks of
+// 4096 to 32768 slots (a chunk's counts are 16-bit numbers), small enough for one workgroup per CU.
+struct EvictPlan {
+  int32_t chunks, chunk_slots;
+  size_t at_hist, at_state, need;
+};
+EvictPlan evict_plan(int64_t rows, int64_t capacity) {
+  EvictPlan p;
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  p.chunks = 0;
+  p.chunk_slots = 0;
+  p.at_hist = p.at_state = p.need = up(rows * sizeof(int32_t));
+  if (capacity <= 16384) return p;
+  int64_t slots = (rows * capacity / CUS + 1023) / 1024 * 1024;
+  slots = slots < 4096 ? 4096 : slots > 32768 ? 32768 : slots;
+  p.chunk_slots = (int32_t)slots;
+  p.chunks = (int32_t)((capacity + slots - 1) / slots);
+  p.at_state = p.at_hist + up((size_t)3 * rows * p.chunks * 2048 * 2);
+  p.need = p.at_state + up((size_t)rows * p.chunks * sizeof(SelectState));
+  return p;
+}
+
 bool same_strides(const int64_t *a, const int64_t *b, int n) { return memcmp(a, b, n * sizeof(int64_t)) == 0; }
 
 }  // namespace
@@ -202,7 +224,7 @@ size_t minf_prefix_attn_workspace_bytes(const minf_queries *x, const minf_kv_cac
 
 size_t minf_cache_evict_workspace_bytes(const minf_kv_cache *cache, int32_t keep) {
   if (check_cache(cache, true, false) != MINF_OK || keep < 1) return 0;
-  return ((size_t)cache->batch * cache->n_kv_heads * sizeof(int32_t) + 255) / 256 * 256;
+  return evict_plan((int64_t)cache->batch * cache->n_kv_heads, cache->capacity).need;
 }
 
 minf_status minf_cache_attn(const minf_queries *x, const minf_kv_cache *cache, int32_t n_init, int32_t n_local,
@@ -252,8 +274,8 @@ minf_status minf_cache_evict(const minf_kv_cache *cache, int32_t n_init, int32_t
       if (lists[i].meets(r)) return MINF_ERR_SHAPE;
     if ((i == 0 || to->lens != cache->lens) && lists[i].meets(lens_range(cache->lens, cache->batch))) return MINF_ERR_SHAPE;
   }
-  const size_t need = minf_cache_evict_workspace_bytes(cache, keep);
-  if (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % 256 != 0) return MINF_ERR_WORKSPACE;
+  const EvictPlan p = evict_plan((int64_t)cache->batch * cache->n_kv_heads, cache->capacity);
+  if (!ws || ws_bytes < p.need || reinterpret_cast<uintptr_t>(ws) % 256 != 0) return MINF_ERR_WORKSPACE;
   EvictCall x;
   x.k = static_cast<const bf16_t *>(cache->k); x.v = static_cast<const bf16_t *>(cache->v);
   x.to_k = static_cast<bf16_t *>(to->k); x.to_v = static_cast<bf16_t *>(to->v);
@@ -267,6 +289,9 @@ minf_status minf_cache_evict(const minf_kv_cache *cache, int32_t n_init, int32_t
   x.tw_sb = to->weight_stride[0]; x.tw_sh = to->weight_stride[1];
   x.batch = cache->batch; x.n_kv = cache->n_kv_heads; x.capacity = cache->capacity; x.to_capacity = to->capacity;
   x.n_init = n_init; x.n_recent = n_recent; x.keep = keep;
+  x.chunks = p.chunks; x.chunk_slots = p.chunk_slots;
+  x.hist = reinterpret_cast<uint32_t *>(static_cast<char *>(ws) + p.at_hist);
+  x.state = reinterpret_cast<SelectState *>(static_cast<char *>(ws) + p.at_state);
   return launch_cache_evict(x, in_place, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? MINF_OK : MINF_ERR_HIP;
 }
 

@@ -10,6 +10,8 @@
 // of 32x32x16 MFMAs (S^T = K Q^T, O^T += V^T P^T, as in the prefill kernels), so P never leaves registers.
 // A segment (row tile of a sequence and K/V head) that several workers share leaves pieces (maximum, sum,
 // unnormalised O) in the workspace, which cache_join_kernel joins.
+#include <type_traits>
+
 #include "cache_walk.h"
 #include "mfma_tile.h"
 
@@ -526,75 +528,227 @@ __device__ inline unsigned weight_key(float v) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int SELECT_THREADS = 1024;
-// Sum of v over the lower threads of the workgroup, and over all of them.  part: SELECT_THREADS / 64 + 1 words.
+constexpr int SELECT_THREADS = 1024, SELECT_WAVES = SELECT_THREADS / 64;
+constexpr int SELECT_BINS = 2048, SELECT_COPIES = 4;
+// The kept weight of rank `want` is found digit by digit: 11, 11 and 10 bits from the most significant one.
+__device__ constexpr int select_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ constexpr int select_bins(int pass) { return pass == 2 ? 1024 : 2048; }
+__device__ constexpr unsigned select_mask(int pass) { return pass == 0 ? 0u : ~0u << select_shift(pass - 1); }
+
+// Sum of v over the lower threads of the workgroup, and over all of them.
 __device__ inline int block_scan(int v, int *part, int &all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockDim.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int incl = wave_scan(v, lane);
   __syncthreads();
   if (lane == 63) part[wave] = incl;
   __syncthreads();
   int before = 0;
   all = 0;
-  for (int i = 0; i < n; ++i) {
-    if (i < wave) before += part[i];
-    all += part[i];
+#pragma unroll
+  for (int i = 0; i < SELECT_WAVES; ++i) {
+    const int p = part[i];
+    if (i < wave) before += p;
+    all += p;
   }
   return before + incl - v;
 }
 
-// Kept slots of one sequence and K/V head: the keep largest weights in four passes over eight bits each, from
-// the most significant one; then the slots in ascending order.
+// One sequence and K/V head.
+struct SelectRow {
+  const float *w;
+  int len, first, last;          // tokens; slots first .. last - 1 are chosen by weight
+  int want;                      // ... so many of them
+  __device__ inline SelectRow(const EvictCall &x, int row) {
+    const int b = row / x.n_kv, kvh = row - b * x.n_kv;
+    w = x.weight + b * x.w_sb + kvh * x.w_sh;
+    len = min(max(x.lens[b], 0), x.capacity);
+    first = x.n_init; last = len - x.n_recent;
+    want = x.keep - x.n_init - x.n_recent;
+  }
+};
+
+struct SelectLds {
+  int hist[SELECT_COPIES][SELECT_BINS];
+  int part[SELECT_WAVES], pick[3];
+};
+
+// Histogram of the pass's digit over the slots from .. to - 1 whose higher digits are those of `prefix`.  Lanes
+// add into four copies: weights cluster, and lanes that meet in a bin go one after the other.
+template <int PASS>
+__device__ inline void select_count(const SelectRow &r, int from, int to, unsigned prefix, SelectLds &s) {
+  const int tid = threadIdx.x;
+  for (int i = tid; i < SELECT_COPIES * SELECT_BINS; i += SELECT_THREADS) (&s.hist[0][0])[i] = 0;
+  __syncthreads();
+  from = max(from, r.first);
+  to = min(to, r.last);
+#pragma unroll 4
+  for (int i = from + tid; i < to; i += SELECT_THREADS) {
+    const unsigned k = weight_key(r.w[i]);
+    if ((k & select_mask(PASS)) == prefix) atomicAdd(&s.hist[tid & (SELECT_COPIES - 1)][(k >> select_shift(PASS)) & (select_bins(PASS) - 1)], 1);
+  }
+  __syncthreads();
+}
+
+// The digit of rank `want` from this thread's two bins (2047 - 2 tid and the one below: descending), and the
+// number of slots above it: in all, and in the chunks before this one (n_before).  Lowers `want` to the rank
+// among the slots with that digit.
+__device__ inline unsigned select_pick(const int (&n)[2], const int (&n_before)[2], int bins, int &want, int &gt_before,
+                                       int &eq_before, SelectLds &s) {
+  const int hi = bins - 1 - 2 * (int)threadIdx.x;
+  int all;
+  const int above = block_scan(n[0] + n[1], s.part, all);
+  if (above < want && want <= above + n[0] + n[1]) {
+    const int lower = above + n[0] < want;
+    s.pick[0] = hi - lower;
+    s.pick[1] = above + (lower ? n[0] : 0);
+    s.pick[2] = n_before[lower];
+  }
+  __syncthreads();
+  const int d = s.pick[0];
+  eq_before = s.pick[2];
+  want -= s.pick[1];
+  block_scan((hi > d ? n_before[0] : 0) + (hi - 1 > d ? n_before[1] : 0), s.part, gt_before);
+  return (unsigned)d;
+}
+
+// Writes the kept slots among from .. to - 1 (a wave takes consecutive ones) behind the `gt` larger and `eq`
+// equal ones of lower slots; of the equal ones the first `want` stay.
+__device__ inline void select_emit(const SelectRow &r, int from, int to, unsigned key, int want, int gt, int eq, int32_t *kept,
+                                   int keep, SelectLds &s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (to - from + SELECT_THREADS - 1) / SELECT_THREADS * 64;
+  const int w0 = from + wave * per, w1 = min(w0 + per, min(to, r.last));
+  const unsigned long long below = (1ull << lane) - 1;
+  auto look = [&](int i, unsigned long long &g, unsigned long long &e) {
+    const bool in = i >= r.first && i < w1;
+    const unsigned k = in ? weight_key(r.w[i]) : 0u;
+    g = __builtin_amdgcn_ballot_w64(in && k > key);
+    e = __builtin_amdgcn_ballot_w64(in && k == key);
+  };
+  int ng = 0, ne = 0;
+  for (int i0 = w0; i0 < w1; i0 += 64) {
+    unsigned long long g, e;
+    look(i0 + lane, g, e);
+    ng += __popcll(g);
+    ne += __popcll(e);
+  }
+  int all;
+  const int before_g = block_scan(lane == 0 ? ng : 0, s.part, all), before_e = block_scan(lane == 0 ? ne : 0, s.part, all);
+  gt += uni(before_g);
+  eq += uni(before_e);
+  for (int i0 = w0; i0 < w1; i0 += 64) {
+    unsigned long long g, e;
+    look(i0 + lane, g, e);
+    const int gr = gt + __popcll(g & below), er = eq + __popcll(e & below);
+    if ((g >> lane) & 1 || ((e >> lane) & 1 && er < want)) kept[r.first + gr + min(er, want)] = i0 + lane;
+    gt += __popcll(g);
+    eq += __popcll(e);
+  }
+  // the first and the last slots stay whatever they weigh
+  for (int i = from + tid; i < min(to, r.first); i += SELECT_THREADS) kept[i] = i;
+  for (int i = max(from, r.last) + tid; i < min(to, r.len); i += SELECT_THREADS) kept[keep - (r.len - i)] = i;
+}
+
+__device__ inline void select_all(int len, int32_t *kept, int keep, int from, int step) {
+  for (int i = from; i < keep; i += step) kept[i] = i < len ? i : -1;
+}
+
+// Short rows: one workgroup per sequence and K/V head, one launch.
 __global__ __launch_bounds__(SELECT_THREADS) void cache_select_kernel(EvictCall x) {
-  __shared__ int hist[256], part[SELECT_THREADS / 64], pick[2];
-  const int row = blockIdx.x, b = row / x.n_kv, kvh = row - b * x.n_kv, tid = threadIdx.x;
-  const int len = min(max(x.lens[b], 0), x.capacity), n = min(len, x.keep);
+  __shared__ SelectLds s;
+  const int row = blockIdx.x, tid = threadIdx.x;
+  const SelectRow r(x, row);
   int32_t *kept = x.kept + (int64_t)row * x.keep;
-  if (tid == 0) x.counts[row] = n;
-  if (len <= x.keep) {
-    for (int i = tid; i < x.keep; i += SELECT_THREADS) kept[i] = i < len ? i : -1;
-    return;
+  if (tid == 0) x.counts[row] = min(r.len, x.keep);
+  if (r.len <= x.keep) return select_all(r.len, kept, x.keep, tid, SELECT_THREADS);
+  unsigned key = ~0u;                         // above every weight: nothing to choose
+  int want = r.want, gt = 0, eq = 0;
+  if (want > 0) {
+    key = 0;
+    auto pass = [&](auto p) {
+      constexpr int P = decltype(p)::value;
+      select_count<P>(r, 0, r.len, key, s);
+      int n[2] = {0, 0};
+      const int none[2] = {0, 0}, hi = select_bins(P) - 1 - 2 * tid;
+      if (hi > 0)
+        for (int c = 0; c < SELECT_COPIES; ++c) {
+          n[0] += s.hist[c][hi];
+          n[1] += s.hist[c][hi - 1];
+        }
+      key |= select_pick(n, none, select_bins(P), want, gt, eq, s) << select_shift(P);
+    };
+    pass(std::integral_constant<int, 0>{});
+    pass(std::integral_constant<int, 1>{});
+    pass(std::integral_constant<int, 2>{});
   }
-  const float *w = x.weight + b * x.w_sb + kvh * x.w_sh;
-  const int first = x.n_init, last = len - x.n_recent;
-  int want = x.keep - x.n_init - x.n_recent;             // of the slots first .. last - 1
-  unsigned prefix = 0, mask = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += SELECT_THREADS) hist[i] = 0;
-    __syncthreads();
-    for (int i = first + tid; i < last; i += SELECT_THREADS) {
-      const unsigned k = weight_key(w[i]);
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+  select_emit(r, 0, r.len, key, want, 0, 0, kept, x.keep, s);
+}
+
+// Long rows: a row in chunks, a workgroup each.  Pass p counts its digit per chunk; the workgroups of the next
+// launch each add up the row's counts and pick the digit themselves (no atomics on memory, nothing to clear).
+template <int PASS>
+__device__ inline void select_from_counts(const EvictCall &x, int row, int chunk, unsigned &key, int &want, int &gt, int &eq,
+                                          SelectLds &s) {
+  const int hi = select_bins(PASS) - 1 - 2 * (int)threadIdx.x;
+  int n[2] = {0, 0}, before[2] = {0, 0};
+  if (hi > 0) {
+    const unsigned *h = x.hist + (((int64_t)PASS * gridDim.y + row) * x.chunks * SELECT_BINS + (hi - 1)) / 2;
+#pragma unroll 8
+    for (int c = 0; c < x.chunks; ++c) {
+      const unsigned two = h[(int64_t)c * (SELECT_BINS / 2)];
+      n[0] += two >> 16;
+      n[1] += two & 0xffff;
+      before[0] += c < chunk ? two >> 16 : 0;
+      before[1] += c < chunk ? two & 0xffff : 0;
     }
-    __syncthreads();
-    if (tid == 0) {
-      int above = 0, d = 255;
-      while (d > 0 && above + hist[d] < want) above += hist[d--];
-      pick[0] = d;
-      pick[1] = above;
-    }
-    __syncthreads();
-    prefix |= (unsigned)pick[0] << shift;
-    mask |= 255u << shift;
-    want -= pick[1];
-    __syncthreads();
   }
-  // `want` of the slots whose weight equals the last kept one, the lowest ones
-  int out = 0, equal_before = 0;
-  for (int i0 = 0; i0 < len; i0 += SELECT_THREADS) {
-    const int i = i0 + tid;
-    const bool forced = i < first || (i >= last && i < len);
-    const unsigned k = i >= first && i < last ? weight_key(w[i]) : 0u;
-    const bool middle = i >= first && i < last;
-    const bool equal = middle && k == prefix;
-    int equals, takes;
-    const int e = block_scan(equal ? 1 : 0, part, equals);
-    const bool take = forced || (middle && k > prefix) || (equal && equal_before + e < want);
-    const int at = block_scan(take ? 1 : 0, part, takes);
-    if (take) kept[out + at] = i;
-    out += takes;
-    equal_before += equals;
+  int above;
+  key |= select_pick(n, before, select_bins(PASS), want, above, eq, s) << select_shift(PASS);
+  gt += above;
+}
+
+template <int PASS>
+__global__ __launch_bounds__(SELECT_THREADS) void cache_count_kernel(EvictCall x) {
+  __shared__ SelectLds s;
+  const int chunk = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  const SelectRow r(x, row);
+  const int from = chunk * x.chunk_slots, to = min(from + x.chunk_slots, r.len);
+  if (r.len <= x.keep || r.want == 0) return;
+  // digits so far, rank left, larger slots in the chunks before this one
+  SelectState *state = x.state + (int64_t)row * x.chunks + chunk;
+  unsigned key = 0;
+  int want = r.want, gt = 0, eq = 0;
+  if (PASS == 2) { key = state->key; want = state->want; gt = state->gt; }
+  if (PASS > 0) {
+    select_from_counts<PASS == 0 ? 0 : PASS - 1>(x, row, chunk, key, want, gt, eq, s);
+    if (tid == 0) *state = SelectState{key, want, gt};
   }
+  select_count<PASS>(r, from, to, key, s);
+  unsigned *h = x.hist + (((int64_t)PASS * gridDim.y + row) * x.chunks + chunk) * (SELECT_BINS / 2);
+  for (int i = tid; i < select_bins(PASS) / 2; i += SELECT_THREADS) {
+    int a = 0, b = 0;
+#pragma unroll
+    for (int c = 0; c < SELECT_COPIES; ++c) { a += s.hist[c][2 * i]; b += s.hist[c][2 * i + 1]; }
+    h[i] = (unsigned)b << 16 | (unsigned)a;
+  }
+}
+
+__global__ __launch_bounds__(SELECT_THREADS) void cache_emit_kernel(EvictCall x) {
+  __shared__ SelectLds s;
+  const int chunk = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  const SelectRow r(x, row);
+  int32_t *kept = x.kept + (int64_t)row * x.keep;
+  if (chunk == 0 && tid == 0) x.counts[row] = min(r.len, x.keep);
+  if (r.len <= x.keep) return select_all(r.len, kept, x.keep, chunk * SELECT_THREADS + tid, x.chunks * SELECT_THREADS);
+  const int from = chunk * x.chunk_slots, to = min(from + x.chunk_slots, r.len);
+  unsigned key = ~0u;
+  int want = 0, gt = 0, eq = 0;
+  if (r.want > 0) {
+    const SelectState st = x.state[(int64_t)row * x.chunks + chunk];
+    key = st.key; want = st.want; gt = st.gt;
+    select_from_counts<2>(x, row, chunk, key, want, gt, eq, s);
+  }
+  if (from < to) select_emit(r, from, to, key, want, gt, eq, kept, x.keep, s);
 }
 
 // Moves the kept rows to the slots 0, 1, ...  A workgroup owns one slice of 64 bytes of the rows of K or V of
@@ -672,7 +826,15 @@ hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
 
 hipError_t launch_cache_evict(const EvictCall &x, bool in_place, hipStream_t st) {
   const int rows = x.batch * x.n_kv;
-  hipLaunchKernelGGL(cache_select_kernel, dim3(rows), dim3(SELECT_THREADS), 0, st, x);
+  if (x.chunks == 0) {
+    hipLaunchKernelGGL(cache_select_kernel, dim3(rows), dim3(SELECT_THREADS), 0, st, x);
+  } else {
+    const dim3 grid(x.chunks, rows);
+    hipLaunchKernelGGL(cache_count_kernel<0>, grid, dim3(SELECT_THREADS), 0, st, x);
+    hipLaunchKernelGGL(cache_count_kernel<1>, grid, dim3(SELECT_THREADS), 0, st, x);
+    hipLaunchKernelGGL(cache_count_kernel<2>, grid, dim3(SELECT_THREADS), 0, st, x);
+    hipLaunchKernelGGL(cache_emit_kernel, grid, dim3(SELECT_THREADS), 0, st, x);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int chunks = (x.keep + MOVE_ROWS - 1) / MOVE_ROWS;

@@ -241,6 +241,10 @@ struct CacheCall {
 };
 hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st);
 
+struct SelectState {
+  uint32_t key;
+  int32_t want, gt;
+};
 struct EvictCall {
   const bf16_t *k, *v;
   bf16_t *to_k, *to_v;
@@ -250,6 +254,11 @@ struct EvictCall {
   int32_t *to_lens, *kept, *counts;     // counts (workspace) [sequence, K/V head]: kept slots
   int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st, w_sb, w_sh, tk_sb, tk_sh, tk_st, tv_sb, tv_sh, tv_st, tw_sb, tw_sh;
   int32_t batch, n_kv, capacity, to_capacity, n_init, n_recent, keep;
+  // rows in chunks (chunks = 0: one workgroup per row); workspace: counts of the digits, [pass][row][chunk][2048]
+  // 16-bit numbers, and what is known before the last pass, [row][chunk]
+  int32_t chunks, chunk_slots;
+  uint32_t *hist;
+  SelectState *state;
 };
 hipError_t launch_cache_evict(const EvictCall &x, bool in_place, hipStream_t st);
 
