@@ -108,8 +108,9 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   x.c_log2 = scale * 1.4426950408889634f;
   x.rows = x.group * x.n_new;
   const int64_t p_rows = prefix ? (int64_t)x.batch * x.rows : 0;
-  x.wide = (p_rows > x.rows ? p_rows : x.rows) > 32;
-  const int tile_rows = x.wide ? 64 : 32;
+  const int64_t most = p_rows > x.rows ? p_rows : x.rows;
+  x.row_blocks = most <= 16 ? 1 : 2;
+  const int tile_rows = 16 * x.row_blocks;
   x.row_tiles = (x.rows + tile_rows - 1) / tile_rows;
   x.slot_rows = prefix || x.rows > tile_rows ? tile_rows : x.rows;
   // the longest walk: sink and window, each with a tile that it fills in part

@@ -7,8 +7,9 @@
 // the memory bounds it, so the kernel is built to keep loads in flight.  A wave is a worker of its own: it
 // takes a consecutive share of the tiles of all sequences (cache_walk.h), fetches tile t+1 into its half of an
 // LDS ring (global -> LDS, no registers) while it computes tile t, and meets no barrier.  Rows are the columns
-// of 32x32x16 MFMAs (S^T = K Q^T, O^T += V^T P^T, as in the prefill kernels), so P never leaves registers.
-// A segment (row tile of a sequence and K/V head) that several workers share leaves pieces (maximum, sum,
+// of 16x16x32 MFMAs (S^T = K Q^T, O^T += V^T P^T): the accumulator layout of S^T is the operand layout that the
+// second product needs, so P never leaves registers.
+// A segment (row tile of a sequence and K/V head) that several workers share leaves pieces (reference, sum,
 // unnormalised O) in the workspace, which cache_join_kernel joins.
 #include <type_traits>
 
@@ -51,16 +52,12 @@ __device__ inline int wave_scan(int v, int lane) {
   return v;
 }
 
-// Tiles in front of the own segments of sequence b (b = batch: all of them), per K/V head and row tile.
-__device__ inline int tiles_before(const CacheCall &x, int b, int lane) {
+// Tiles of all sequences, per K/V head and row tile.
+__device__ inline int all_tiles(const CacheCall &x, int lane) {
   int sum = 0;
-  for (int b0 = 0; b0 < b; b0 += 64) {
-    const int i = b0 + lane;
-    int t = i < b ? walk_of(x, i).tiles : 0;
+  for (int b0 = 0; b0 < x.batch; b0 += 64) sum += b0 + lane < x.batch ? walk_of(x, b0 + lane).tiles : 0;
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) t += __shfl_xor(t, d);
-    sum += t;
-  }
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   return uni(sum);
 }
 
@@ -121,15 +118,22 @@ __device__ inline int segment_of(const CacheCall &x, const CacheCursor &c) {
 }
 
 // ---- tile arithmetic ------------------------------------------------------------------------------------
-// Rows of a segment: 32 NT per row tile.  Row r of a sequence is token r / group of the n_new, query head
+// Rows of a segment: 16 NB per row tile.  Row r of a sequence is token r / group of the n_new, query head
 // r % group of the K/V head's group; rows of the prefix are those of all sequences, one after the other.
-template <int NT>
+// Lane l = 16 g + n holds, of row n of each block of 16: the query's d = 32 ks + 8 g + (0..7), the logits of the
+// keys 4 g + (0..3) and 16 + 4 g + (0..3) of a tile, O at d = 16 db + 4 g + (0..3).
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <int NB>
+struct CacheQ {
+  bf16x8 q[NB][4];
+};
+template <int NB>
 struct CacheRows {
-  bf16x8 q[NT][8];
-  f32x16 o[NT][4];        // [row half][d block]
-  float m[NT], l[NT];     // running maximum (base 2), this lane's share of the running sum
-  int pos[NT];            // position of this lane's row: it sees the slots up to there
-  int tok[NT];            // its token, 0 .. n_new - 1
+  CacheQ<NB> q;
+  f32x4 o[NB][8];         // [row block][d block]
+  float m[NB], l[NB];     // exponent reference of the row (base 2), this lane's share of the running sum
+  int pos[NB];            // position of this lane's row: it sees the slots up to there
+  int tok[NB];            // its token, 0 .. n_new - 1
 };
 
 struct LaneRow {
@@ -144,27 +148,52 @@ __device__ inline LaneRow lane_row(const CacheCall &x, const CacheCursor &c, int
   a.g = r - a.t * x.group;
   return a;
 }
+// This lane's row of block nb; rows behind the last one repeat it, nobody stores them.
+template <int NB>
+__device__ inline LaneRow block_row(const CacheCall &x, const CacheCursor &c, int nb, int lane) {
+  const int last = (c.prefix ? x.batch * x.rows : x.rows) - 1;
+  return lane_row(x, c, min((c.rt * NB + nb) * 16 + (lane & 15), last));
+}
 
-template <int NT>
-__device__ inline void begin_segment(const CacheCall &x, const CacheCursor &c, CacheRows<NT> &st, int lane) {
-  const int n = lane & 31, h = lane >> 5, last = (c.prefix ? x.batch * x.rows : x.rows) - 1;
+template <int NB>
+__device__ inline void load_queries(const CacheCall &x, const CacheCursor &c, CacheQ<NB> &q, int lane) {
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    // rows behind the last one repeat it; nobody stores them
-    const LaneRow a = lane_row(x, c, min((c.rt * NT + nt) * 32 + n, last));
-    const bf16_t *row = x.q + a.b * x.q_sb + (int64_t)(c.kvh * x.group + a.g) * x.q_sh + a.t * x.q_st + 8 * h;
+  for (int nb = 0; nb < NB; ++nb) {
+    const LaneRow a = block_row<NB>(x, c, nb, lane);
+    const bf16_t *row = x.q + a.b * x.q_sb + (int64_t)(c.kvh * x.group + a.g) * x.q_sh + a.t * x.q_st + 8 * (lane >> 4);
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) st.q[nt][ks] = *reinterpret_cast<const bf16x8 *>(row + 16 * ks);
-    st.tok[nt] = c.prefix ? 0 : a.t;
-    st.pos[nt] = c.prefix ? c.w.len - 1 : c.w.i0 + a.t;
-    st.m[nt] = -INFINITY;
-    st.l[nt] = 0.f;
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) st.o[nt][db][r] = 0.f;
+    for (int ks = 0; ks < 4; ++ks) q.q[nb][ks] = *reinterpret_cast<const bf16x8 *>(row + 32 * ks);
   }
 }
+
+template <int NB>
+__device__ inline void begin_segment(const CacheCall &x, const CacheCursor &c, CacheRows<NB> &st, int lane) {
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const LaneRow a = block_row<NB>(x, c, nb, lane);
+    st.tok[nb] = c.prefix ? 0 : a.t;
+    st.pos[nb] = c.prefix ? c.w.len - 1 : c.w.i0 + a.t;
+    st.m[nb] = -INFINITY;
+    st.l[nb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) st.o[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+
+// Per-lane byte offsets of the MFMA operands in a tile (layout: mfma_tile.h).
+struct CacheLane {
+  int k[4];        // k step ks of key lane % 16; the second 16 keys lie 16 rows further, at the same swizzle
+  int v[8];        // d block db of the keys 4 g .. 4 g + 3, transposed on reading
+  __device__ inline void init(int lane) {
+    const int n = lane & 15, g = lane >> 4, j = n >> 2, c = n & 3;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) k[ks] = swz_byte(n, 4 * ks + g);
+#pragma unroll
+    for (int db = 0; db < 8; ++db) v[db] = swz_byte(4 * g + j, 2 * db + (c >> 1)) + (c & 1) * 8;
+  }
+};
+constexpr int HALF_TILE_ROWS = 16 * ROW_BYTES;
+__device__ inline int lane_key(int lane, int e) { return 4 * (lane >> 4) + (e & 3) + 16 * (e >> 2); }
 
 __device__ inline bool tile_not_finite(const char *tV, int lane) {
   bool bad = false;
@@ -181,242 +210,275 @@ __device__ inline bool tile_not_finite(const char *tV, int lane) {
 
 // O^T += V^T P^T for the tokens one by one, with the V rows that a token does not see as zeros: 0 * inf and
 // 0 * NaN of a slot that a row's mask excludes would otherwise reach the row.  Only tiles with a mask and
-// with such values take it.
-template <int NT>
-__device__ inline void update_by_token(CacheRows<NT> &st, const bf16x8 (&p)[NT][2][2],
-                                                          const char *tV, int kb, int n_tok, int first_pos,
-                                                          int n_init, int n_local, int lane) {
-  LaneOfs lo;
-  lane_offsets(lo, lane);
-  const int h = lane >> 5;
-  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-  for (int t = 0; t < n_tok; ++t) {
-    unsigned sees[2] = {0u, 0u};
+// with such values take it.  O goes through 8 KiB of LDS (`room`, the K tile that is no longer needed), so
+// that this rare path costs the others no registers.
+template <int NB>
+__device__ inline void update_by_token(CacheRows<NB> &st, const bf16x8 (&p)[NB][2], const CacheLane &lo, const char *tV, char *room,
+                                       int kb, int n_tok, int first_pos, int n_init, int n_local, int lane) {
+  f32x4 *mine = reinterpret_cast<f32x4 *>(room) + lane;
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
+  for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+    for (int db = 0; db < 8; ++db) mine[64 * db] = st.o[nb][db];
+#pragma unroll 1
+    for (int i = 0; i < 8 * n_tok; ++i) {
+      const int db = i & 7, t = i >> 3;
+      const int at = swz_byte(4 * (lane >> 4) + ((lane & 15) >> 2), 2 * db + ((lane & 3) >> 1)) + (lane & 1) * 8;
+      s16x8 w = __builtin_bit_cast(s16x8, lds_read_vt(tV, at, at + HALF_TILE_ROWS));
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (cache_visible(kb + 16 * tt + 8 * h + e, first_pos + t, n_init, n_local)) sees[tt] |= 1u << e;
-#pragma unroll
-    for (int db = 0; db < 4; ++db) {
-      bf16x8 a[2];
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        s16x8 w = __builtin_bit_cast(s16x8, lds_read_vt(tV, lo.v[db][0] + 16 * tt * ROW_BYTES,
-                                                        lo.v[db][1] + 16 * tt * ROW_BYTES));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = (sees[tt] >> e) & 1 ? w[e] : (short)0;
-        a[tt] = __builtin_bit_cast(bf16x8, w);
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        f32x16 add = zero;
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int part = 0; part < 2; ++part)
-            add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[tt], p[nt][tt][part], add, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) st.o[nt][db][r] += st.tok[nt] == t ? add[r] : 0.f;
-      }
+        w[e] = cache_visible(kb + lane_key(lane, e), first_pos + t, n_init, n_local) ? w[e] : (short)0;
+      const bf16x8 a = __builtin_bit_cast(bf16x8, w);
+      f32x4 add = {0.f, 0.f, 0.f, 0.f};
+      add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][0], add, 0, 0, 0);
+      add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][1], add, 0, 0, 0);
+      if (st.tok[nb] == t) mine[64 * db] += add;
     }
+#pragma unroll
+    for (int db = 0; db < 8; ++db) st.o[nb][db] = mine[64 * db];
   }
 }
 
-// One tile of 32 keys from slot kb on.  Register r of s holds key 16 (r / 8) + 8 h + r % 8 of row n.
-template <int NT>
-__device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, CacheRows<NT> &st, const LaneOfs &lo,
-                                  const char *tK, const char *tV, int lane) {
-  const int n = lane & 31, h = lane >> 5, kb = c.w.base(c.tau);
-  f32x16 s[NT];
+// A row's exponent reference is its maximum when it was last taken; logits may outgrow it by REF_ROOM (2^16 in
+// the sums, far from any limit of fp32) before it is taken anew.  So nearly every tile needs no maximum
+// across lanes and no rescaling.
+constexpr float REF_ROOM = 16.f;
+
+// One tile of 32 keys.  WAIT_V: awaits the V tile (the K tile is there).
+template <int NB, class WaitV>
+__device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, CacheRows<NB> &st, const CacheLane &lo,
+                                  char *tK, const char *tV, int lane, WaitV wait_v) {
+  const int kb = c.w.base(c.tau);
+  f32x4 s[NB][2];
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks) {
-    const bf16x8 a = lds_read_k(tK, lo.k[ks]);
+  for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      s[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, st.q[nt][ks], ks == 0 ? zero : s[nt], 0, 0, 0);
+    for (int kt = 0; kt < 2; ++kt) {
+      const bf16x8 a = lds_read_k(tK, lo.k[ks] + kt * HALF_TILE_ROWS);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        s[nb][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, st.q.q[nb][ks], ks == 0 ? zero : s[nb][kt], 0, 0, 0);
+      }
     }
-  }
   const int n_init = c.prefix ? 0 : x.n_init, n_local = c.prefix ? x.p_cap : x.n_local;
   const int first_pos = c.prefix ? c.w.len - 1 : c.w.i0, last_pos = c.w.len - 1, klast = kb + CACHE_TILE - 1;
   const bool whole = klast <= first_pos && (klast < n_init || last_pos - kb < n_local);
   if (!whole) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int key = kb + 16 * (r >> 3) + 8 * h + (r & 7);
-        s[nt][r] = cache_visible(key, st.pos[nt], n_init, n_local) ? s[nt][r] : -INFINITY;
-      }
+      for (int e = 0; e < 8; ++e)
+        s[nb][e >> 2][e & 3] = cache_visible(kb + lane_key(lane, e), st.pos[nb], n_init, n_local) ? s[nb][e >> 2][e & 3] : -INFINITY;
   }
-  if (x.logits && !c.prefix) {
-    float *row0 = x.logits + (((int64_t)c.b * x.n_kv + c.kvh) * x.max_tiles + c.tau) * (x.rows * CACHE_TILE);
+  bool outgrown = false;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = (c.rt * NT + nt) * 32 + n;
-      if (row < x.rows) {
+  for (int nb = 0; nb < NB; ++nb) {
+    float mx = s[nb][0][0];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 w = {s[nt][4 * i] * x.c_log2, s[nt][4 * i + 1] * x.c_log2, s[nt][4 * i + 2] * x.c_log2,
-                            s[nt][4 * i + 3] * x.c_log2};
-          *reinterpret_cast<float4 *>(row0 + row * CACHE_TILE + 16 * (i >> 1) + 8 * h + 4 * (i & 1)) = w;
-        }
-      }
-    }
+    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[nb][e >> 2][e & 3]);
+    outgrown = outgrown || mx * x.c_log2 > st.m[nb] + REF_ROOM;
   }
-  // running maximum; the sums and O follow only where a row's maximum grew
-  float m_new[NT];
-  bool grew = false;
+  if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    float mx = s[nt][0];
+    for (int nb = 0; nb < NB; ++nb) {
+      float mx = s[nb][0][0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[nt][r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32)) * x.c_log2;
-    m_new[nt] = fmaxf(st.m[nt], mx);
-    grew = grew || m_new[nt] > st.m[nt];
-  }
-  if (__builtin_amdgcn_ballot_w64(grew) != 0) {
+      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[nb][e >> 2][e & 3]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) * x.c_log2;
+      const float m_new = fmaxf(st.m[nb], mx);
+      const float f = m_new == -INFINITY ? 1.f : fast_exp2(st.m[nb] - m_new);
+      st.m[nb] = m_new;
+      st.l[nb] *= f;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const float f = m_new[nt] == -INFINITY ? 1.f : fast_exp2(st.m[nt] - m_new[nt]);
-      st.m[nt] = m_new[nt];
-      st.l[nt] *= f;
-#pragma unroll
-      for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) st.o[nt][db][r] *= f;
+      for (int db = 0; db < 8; ++db) st.o[nb][db] *= f;
     }
   }
   // P as the sum of two bf16 (16 bits of mantissa): the matrix cores idle here, and the output is then as
   // good as from fp32 weights
-  bf16x8 p[NT][2][2];
+  bf16x8 p[NB][2];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const float m = st.m[nt] == -INFINITY ? 0.f : st.m[nt];
+  for (int nb = 0; nb < NB; ++nb) {
+    const float m = st.m[nb] == -INFINITY ? 0.f : st.m[nb];
+    float sum = 0.f;
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = fast_exp2(fmaf(s[nt][8 * tt + e], x.c_log2, -m));
-        st.l[nt] += v;
-        const __bf16 hi = (__bf16)v;
-        p[nt][tt][0][e] = hi;
-        p[nt][tt][1][e] = (__bf16)(v - (float)hi);
-      }
+    for (int e = 0; e < 8; e += 2) {
+      const f32x2 v = {fast_exp2(fmaf(s[nb][e >> 2][e & 3], x.c_log2, -m)), fast_exp2(fmaf(s[nb][e >> 2][(e & 3) + 1], x.c_log2, -m))};
+      sum += v[0] + v[1];
+      const bf16x2 hi = __builtin_convertvector(v, bf16x2);
+      const f32x2 rest = {v[0] - (float)hi[0], v[1] - (float)hi[1]};
+      const bf16x2 lw = __builtin_convertvector(rest, bf16x2);
+      p[nb][0][e] = hi[0]; p[nb][0][e + 1] = hi[1];
+      p[nb][1][e] = lw[0]; p[nb][1][e + 1] = lw[1];
+    }
+    st.l[nb] += sum;
   }
+  wait_v();
   if (!whole && tile_not_finite(tV, lane)) {
-    update_by_token<NT>(st, p, tV, kb, c.prefix ? 1 : x.n_new, first_pos, n_init, n_local, lane);
-    return;
-  }
+    update_by_token<NB>(st, p, lo, tV, tK, kb, c.prefix ? 1 : x.n_new, first_pos, n_init, n_local, lane);
+  } else {
 #pragma unroll
-  for (int tt = 0; tt < 2; ++tt)
+    for (int db = 0; db < 8; ++db) {
+      const bf16x8 a = lds_read_vt(tV, lo.v[db], lo.v[db] + HALF_TILE_ROWS);
 #pragma unroll
-    for (int db = 0; db < 4; ++db) {
-      const bf16x8 a = lds_read_vt(tV, lo.v[db][0] + 16 * tt * ROW_BYTES, lo.v[db][1] + 16 * tt * ROW_BYTES);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int part = 0; part < 2; ++part)
-          st.o[nt][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[nt][tt][part], st.o[nt][db], 0, 0, 0);
+          st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][part], st.o[nb][db], 0, 0, 0);
     }
+  }
+  if (x.logits && !c.prefix) {
+    float *row0 = x.logits + (((int64_t)c.b * x.n_kv + c.kvh) * x.max_tiles + c.tau) * (x.rows * CACHE_TILE) + 4 * (lane >> 4);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int row = (c.rt * NB + nb) * 16 + (lane & 15);
+      if (row < x.rows) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) *reinterpret_cast<f32x4 *>(row0 + row * CACHE_TILE + 16 * kt) = s[nb][kt] * x.c_log2;
+      }
+    }
+  }
 }
 
 // End of a worker's part of a segment: rows of O that are final go out, others into the workspace.
-template <int NT>
-__device__ inline void end_segment(const CacheCall &x, const CacheCursor &c, const CacheRows<NT> &st, bool whole,
+template <int NB>
+__device__ inline void end_segment(const CacheCall &x, const CacheCursor &c, const CacheRows<NB> &st, bool whole,
                                    int slot, int lane) {
-  const int n = lane & 31, h = lane >> 5, rows = c.prefix ? x.batch * x.rows : x.rows;
+  const int n = lane & 15, g = lane >> 4, rows = c.prefix ? x.batch * x.rows : x.rows;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int row = (c.rt * NT + nt) * 32 + n;
-    const float l = st.l[nt] + __shfl_xor(st.l[nt], 32);
+  for (int nb = 0; nb < NB; ++nb) {
+    const int row = (c.rt * NB + nb) * 16 + n;
+    float l = st.l[nb] + __shfl_xor(st.l[nb], 16);
+    l += __shfl_xor(l, 32);
     if (row >= rows) continue;
     if (whole && x.p_cap == 0) {
       const LaneRow a = lane_row(x, c, row);
       const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
-      bf16_t *to = x.o + a.b * x.o_sb + (int64_t)(c.kvh * x.group + a.g) * x.o_sh + a.t * x.o_st + 4 * h;
+      bf16_t *to = x.o + a.b * x.o_sb + (int64_t)(c.kvh * x.group + a.g) * x.o_sh + a.t * x.o_st + 4 * g;
 #pragma unroll
-      for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x2 u = {st.o[nt][db][4 * g] * inv, st.o[nt][db][4 * g + 1] * inv};
-          const f32x2 w = {st.o[nt][db][4 * g + 2] * inv, st.o[nt][db][4 * g + 3] * inv};
-          uint2 two;
-          two.x = __builtin_bit_cast(unsigned, __builtin_convertvector(u, bf16x2));
-          two.y = __builtin_bit_cast(unsigned, __builtin_convertvector(w, bf16x2));
-          *reinterpret_cast<uint2 *>(to + 32 * db + 8 * g) = two;
-        }
-      if (x.stat && h == 0) x.stat[((int64_t)c.b * x.n_kv + c.kvh) * x.rows + row] = float2{st.m[nt], inv};
+      for (int db = 0; db < 8; ++db) {
+        const f32x4 r = st.o[nb][db] * inv;
+        const f32x2 u = {r[0], r[1]}, w = {r[2], r[3]};
+        uint2 two;
+        two.x = __builtin_bit_cast(unsigned, __builtin_convertvector(u, bf16x2));
+        two.y = __builtin_bit_cast(unsigned, __builtin_convertvector(w, bf16x2));
+        *reinterpret_cast<uint2 *>(to + 16 * db) = two;
+      }
+      if (x.stat && g == 0) x.stat[((int64_t)c.b * x.n_kv + c.kvh) * x.rows + row] = float2{st.m[nb], inv};
       continue;
     }
-    const int64_t at = (int64_t)slot * x.slot_rows + nt * 32 + n;
-    if (h == 0) x.piece_ml[at] = float2{st.m[nt], l};
-    float *to = x.piece_o + at * D + 4 * h;
+    const int64_t at = (int64_t)slot * x.slot_rows + nb * 16 + n;
+    if (g == 0) x.piece_ml[at] = float2{st.m[nb], l};
+    float *to = x.piece_o + at * D + 4 * g;
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 w = {st.o[nt][db][4 * g], st.o[nt][db][4 * g + 1], st.o[nt][db][4 * g + 2], st.o[nt][db][4 * g + 3]};
-        *reinterpret_cast<float4 *>(to + 32 * db + 8 * g) = w;
-      }
+    for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(to + 16 * db) = st.o[nb][db];
   }
 }
 
-template <int NT>
+// Where a worker's tile loads come from: bases of the segment's K/V head, and the lanes' offsets inside 16 rows.
+struct CacheSource {
+  const char *kh, *vh;
+  unsigned k_rb, v_rb;                 // bytes between rows
+  unsigned kofs[4], vofs[4];
+  __device__ static inline void lanes(unsigned (&ofs)[4], unsigned rb, int lane) {
+    // the four 1 KiB blocks of 16 rows share a base and differ by the loads' immediate offset, which shifts the
+    // global and the LDS address alike: block j has its row distance less 1024 j here
+    const unsigned rl = lane >> 4, cpos = lane & 15;
+#pragma unroll
+    for (unsigned j = 0; j < 4; ++j) ofs[j] = (4 * j + rl) * rb + (((cpos ^ (rl << 2)) ^ j) << 4) - 1024 * j;
+  }
+  __device__ inline void strides(const CacheCall &x, int prefix, int lane) {
+    k_rb = (unsigned)(prefix ? x.pk_st : x.k_st) * 2u;
+    v_rb = (unsigned)(prefix ? x.pv_st : x.v_st) * 2u;
+    lanes(kofs, k_rb, lane);
+    lanes(vofs, v_rb, lane);
+  }
+  __device__ inline void heads(const CacheCall &x, const CacheCursor &c) {
+    kh = reinterpret_cast<const char *>(c.prefix ? x.pk + c.kvh * x.pk_sh : x.k + c.b * x.k_sb + c.kvh * x.k_sh);
+    vh = reinterpret_cast<const char *>(c.prefix ? x.pv + c.kvh * x.pv_sh : x.v + c.b * x.v_sb + c.kvh * x.v_sh);
+  }
+  // 32 rows from kb on into the tile at lds; rows behind the last token repeat it (masked, and in bounds)
+  __device__ static inline void tile(const char *h, unsigned rb, const unsigned (&ofs)[4], int kb, int len, unsigned lds, int lane) {
+    if (kb + CACHE_TILE <= len) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const char *row0 = h + (uint64_t)(unsigned)(kb + 16 * half) * rb;
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                     "global_load_lds_dwordx4 %0, %1\n\t"
+                     "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
+                     "global_load_lds_dwordx4 %5, %1 offset:3072"
+                     :: "v"(ofs[0]), "s"(row0), "s"(lds + 4096 * half), "v"(ofs[1]), "v"(ofs[2]), "v"(ofs[3]) : "memory");
+      }
+      return;
+    }
+    const int rl = lane >> 4, cpos = lane & 15;
+#pragma unroll
+    for (int blk = 0; blk < 8; ++blk) {
+      const int r = 4 * blk + rl;
+      dma16(h + (uint64_t)(unsigned)min(kb + r, len - 1) * rb + ((cpos ^ swz_f(r)) << 4), lds + blk * 1024);
+    }
+  }
+  __device__ inline void fetch(int kb, int len, unsigned lds, int lane) const {
+    tile(kh, k_rb, kofs, kb, len, lds, lane);
+    tile(vh, v_rb, vofs, kb, len, lds + HALF_BYTES, lane);
+  }
+};
+
+template <int NB>
 __global__ __launch_bounds__(64 * CACHE_WAVES) void cache_attn_kernel(CacheCall x) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   const int worker = blockIdx.x * CACHE_WAVES + wave;
   char *ring = lds + wave * CACHE_RING;
+  const unsigned ring_at = uni(lds_addr_of(ring));
 
   const int pre = prefix_walk(x).tiles * x.n_kv * x.p_row_tiles;
-  const int total = pre + tiles_before(x, x.batch, lane) * x.n_kv * x.row_tiles;
+  const int total = pre + all_tiles(x, lane) * x.n_kv * x.row_tiles;
   const int share = worker_share(total, x.workers, x.min_tiles);
   const int g0 = worker * share, g1 = min(g0 + share, total);
   if (g0 >= g1) return;
 
   CacheCursor cur, nxt;
   seek(x, g0, pre, cur, lane);
-  LaneOfs lo;
-  lane_offsets(lo, lane);
-  auto fetch = [&](const CacheCursor &c, int slot) {
-    DmaLane dl;
-    const int kb = c.w.base(c.tau);
-    char *tK = ring + slot * 2 * HALF_BYTES;
-    const int64_t k_st = c.prefix ? x.pk_st : x.k_st, v_st = c.prefix ? x.pv_st : x.v_st;
-    const bf16_t *kh = c.prefix ? x.pk + c.kvh * x.pk_sh : x.k + c.b * x.k_sb + c.kvh * x.k_sh;
-    const bf16_t *vh = c.prefix ? x.pv + c.kvh * x.pv_sh : x.v + c.b * x.v_sb + c.kvh * x.v_sh;
-    dma_lane_init(dl, k_st, lane);
-    dma_rows<1, 32, true>(kh, k_st, dl, kb, nullptr, c.w.len, tK, 0, lane);
-    dma_lane_init(dl, v_st, lane);
-    dma_rows<1, 32, true>(vh, v_st, dl, kb, nullptr, c.w.len, tK + HALF_BYTES, 0, lane);
-  };
-  CacheRows<NT> st;
-  fetch(cur, 0);
+  CacheSource src;
+  src.strides(x, cur.prefix, lane);
+  src.heads(x, cur);
+  CacheRows<NB> st;
+  CacheQ<NB> q;                              // rows of the next segment, loaded ahead of its first tile (loads return in order)
+  load_queries<NB>(x, cur, st.q, lane);
+  src.fetch(cur.w.base(cur.tau), cur.w.len, ring_at, lane);
+  CacheLane lo;
+  lo.init(lane);
   int piece_t0 = cur.tau;                    // first tile of this worker's part of the segment
-  begin_segment<NT>(x, cur, st, lane);
+  begin_segment<NB>(x, cur, st, lane);
   for (int g = g0, slot = 0;; ++g, slot ^= 1) {
     nxt = cur;
     const bool more = g + 1 < g1 && advance(x, nxt);
     if (more) {
-      fetch(nxt, slot ^ 1);
-      MINF_WAIT_VMCNT(16);                   // the 16 loads just issued may still run, the tile's own have landed
+      if (nxt.tau == 0) {                    // the next segment's rows, ahead of its first tile
+        if (nxt.prefix != cur.prefix) src.strides(x, nxt.prefix, lane);
+        src.heads(x, nxt);
+        load_queries<NB>(x, nxt, q, lane);
+      }
+      src.fetch(nxt.w.base(nxt.tau), nxt.w.len, ring_at + (slot ^ 1) * (2 * HALF_BYTES), lane);
+      MINF_WAIT_VMCNT(24);                   // of the tile before: K has landed
     } else {
-      MINF_WAIT_VMCNT(0);
+      MINF_WAIT_VMCNT(8);
     }
-    const char *tK = ring + slot * 2 * HALF_BYTES;
-    cache_tile<NT>(x, cur, st, lo, tK, tK + HALF_BYTES, lane);
+    char *tK = ring + slot * 2 * HALF_BYTES;
+    cache_tile<NB>(x, cur, st, lo, tK, tK + HALF_BYTES, lane, [&]() {
+      if (more) MINF_WAIT_VMCNT(16); else MINF_WAIT_VMCNT(0);
+    });
     __builtin_amdgcn_s_waitcnt(0xC07F);      // LDS reads done: the slot may be filled again
-    const bool done = !more || nxt.tau == 0;
-    if (done) {
+    if (!more || nxt.tau == 0) {
       const bool whole = piece_t0 == 0 && cur.tau == cur.w.tiles - 1;
       const int first_g = g - (cur.tau - piece_t0);
-      end_segment<NT>(x, cur, st, whole, whole ? 2 * x.workers + segment_of(x, cur) : 2 * worker + (first_g > g0 ? 1 : 0), lane);
+      end_segment<NB>(x, cur, st, whole, whole ? 2 * x.workers + segment_of(x, cur) : 2 * worker + (first_g > g0 ? 1 : 0), lane);
       if (!more) break;
-      begin_segment<NT>(x, nxt, st, lane);
+      st.q = q;
+      begin_segment<NB>(x, nxt, st, lane);
       piece_t0 = 0;
     }
     cur = nxt;
@@ -425,7 +487,9 @@ __global__ __launch_bounds__(64 * CACHE_WAVES) void cache_attn_kernel(CacheCall 
 
 // ---- joining the pieces ---------------------------------------------------------------------------------
 // One workgroup per output row: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the pieces of the row's
-// own segment and of the prefix's.  Rows without a visible key, or without a token, give zeros.
+// own segment and of the prefix's.  A wave takes every fourth piece: first the references and sums of up to 64
+// of them at once (a lane each), then their O rows (two d a lane).  Rows without a visible key, or without a
+// token, give zeros.
 constexpr int JOIN_WAVES = 4;
 __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x, int tile_rows) {
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
@@ -433,39 +497,69 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   const int b = seg / x.n_kv, kvh = seg - b * x.n_kv;
   const int pt = prefix_walk(x).tiles, pre = pt * x.n_kv * x.p_row_tiles;
   const int heads = x.n_kv * x.row_tiles;
-  const int before = tiles_before(x, b, lane);
-  const int total = pre + tiles_before(x, x.batch, lane) * heads;
-  const int share = worker_share(total, x.workers, x.min_tiles);
+  int before = 0, all = 0;
+  for (int b0 = 0; b0 < x.batch; b0 += 64) {
+    const int i = b0 + lane, t = i < x.batch ? walk_of(x, i).tiles : 0;
+    all += t;
+    before += i < b ? t : 0;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    all += __shfl_xor(all, d);
+    before += __shfl_xor(before, d);
+  }
+  const int share = worker_share(uni(pre + all * heads), x.workers, x.min_tiles);
   const SeqWalk w = walk_of_uniform(x, b);
   const int t = row / x.group, rt = row / tile_rows;
   const bool token = w.i0 + t >= 0;
-  const int own0 = pre + before * heads + (kvh * x.row_tiles + rt) * w.tiles;
+  const int own0 = uni(pre + before * heads + (kvh * x.row_tiles + rt) * w.tiles);
   if (x.p_cap == 0 && w.tiles > 0) {
     const SegmentPieces p = segment_pieces(own0, own0 + w.tiles, share);
     if (p.first == p.last) return;                                     // written by the worker itself
   }
   float m = -INFINITY, l = 0.f;
   f32x2 o = {0.f, 0.f};
-  auto add = [&](int64_t at) {
-    const float2 ml = x.piece_ml[at];
-    const f32x2 po = *reinterpret_cast<const f32x2 *>(x.piece_o + at * D + 2 * lane);
-    if (ml.x == -INFINITY && ml.y == 0.f) return;                      // no visible key in the piece
-    const float mn = fmaxf(m, ml.x);
-    const float f = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - mn), g = fast_exp2(ml.x - mn);
-    m = mn;
-    l = l * f + ml.y * g;
-    o[0] = o[0] * f + po[0] * g;
-    o[1] = o[1] * f + po[1] * g;
+  // pieces from, from + JOIN_WAVES, ... to of a segment
+  auto add = [&](int from, int to, auto place) {
+    for (int i0 = from; i0 <= to; i0 += 64 * JOIN_WAVES) {
+      const int n = min(64, (to - i0) / JOIN_WAVES + 1), i = i0 + JOIN_WAVES * min(lane, n - 1);
+      float2 ml = x.piece_ml[place(i)];
+      if (lane >= n) ml = float2{-INFINITY, 0.f};
+      float mx = ml.x;
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+      mx = fmaxf(mx, m);
+      // a piece without a visible key (reference and sum as at its start) counts for nothing
+      const float f = ml.x == -INFINITY && ml.y == 0.f ? 0.f : fast_exp2(ml.x - mx);
+      float sum = f == 0.f ? 0.f : ml.y * f;
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+      const float keep = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - mx);
+      m = mx;
+      l = l * keep + sum;
+      o *= keep;
+      for (int j0 = 0; j0 < n; j0 += 8) {                              // eight loads in flight
+        f32x2 po[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          po[j] = *reinterpret_cast<const f32x2 *>(x.piece_o + place(i0 + JOIN_WAVES * min(j0 + j, n - 1)) * D + 2 * lane);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float fj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), j0 + j));
+          o[0] += fj == 0.f ? 0.f : po[j][0] * fj;                     // lanes behind the last piece hold 0
+          o[1] += fj == 0.f ? 0.f : po[j][1] * fj;
+        }
+      }
+    }
   };
   auto join = [&](int t0, int tiles, int in_tile, int segment) {
     if (tiles <= 0) return;
     const SegmentPieces p = segment_pieces(t0, t0 + tiles, share);
     if (p.first == p.last) {
-      if (wave == 0) add((int64_t)(2 * x.workers + segment) * x.slot_rows + in_tile);
+      if (wave == 0) add(0, 0, [&](int) { return (int64_t)(2 * x.workers + segment) * x.slot_rows + in_tile; });
       return;
     }
-    for (int i = p.first + wave; i <= p.last; i += JOIN_WAVES)
-      add((int64_t)piece_slot(i, t0, share) * x.slot_rows + in_tile);
+    add(p.first + wave, p.last, [&](int i) { return (int64_t)piece_slot(i, t0, share) * x.slot_rows + in_tile; });
   };
   if (token) {
     join(own0, w.tiles, row - rt * tile_rows, x.n_kv * x.p_row_tiles + (b * x.n_kv + kvh) * x.row_tiles + rt);
@@ -502,7 +596,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
 // Weight of every slot: the column sums of the softmax, from the logits that the workers left.
 __global__ __launch_bounds__(256) void cache_weight_kernel(CacheCall x) {
   const int slot = blockIdx.x * 256 + threadIdx.x, kvh = blockIdx.y, b = blockIdx.z;
-  const SeqWalk w = walk_of(x, b);
+  const SeqWalk w = walk_of_uniform(x, b);
   if (slot >= w.len) return;
   const int tau = w.tile_of(slot);
   float sum = 0.f;
@@ -510,6 +604,7 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(CacheCall x) {
     const int64_t head = (int64_t)b * x.n_kv + kvh;
     const float *s = x.logits + (head * x.max_tiles + tau) * (x.rows * CACHE_TILE) + (slot - w.base(tau));
     const float2 *st = x.stat + head * x.rows;
+#pragma unroll 8
     for (int r = 0; r < x.rows; ++r) {
       const float v = s[r * CACHE_TILE];
       const float2 ml = st[r];
@@ -804,21 +899,20 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictCall x, int in_pla
 }
 
 // ---- host-side launches -------------------------------------------------------------------------------------
-template <int NT>
+template <int NB>
 static hipError_t launch_workers(const CacheCall &x, hipStream_t st) {
   const size_t lds = CACHE_WAVES * CACHE_RING;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_attn_kernel<NT>),
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_attn_kernel<NB>),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(cache_attn_kernel<NT>, dim3(x.workers / CACHE_WAVES), dim3(64 * CACHE_WAVES), lds, st, x);
+  hipLaunchKernelGGL(cache_attn_kernel<NB>, dim3(x.workers / CACHE_WAVES), dim3(64 * CACHE_WAVES), lds, st, x);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
-  hipError_t e = x.wide ? launch_workers<2>(x, st) : launch_workers<1>(x, st);
+  hipError_t e = x.row_blocks == 1 ? launch_workers<1>(x, st) : launch_workers<2>(x, st);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(cache_join_kernel, dim3(x.batch * x.n_kv * x.rows), dim3(64 * JOIN_WAVES), 0, st, x,
-                     x.wide ? 64 : 32);
+  hipLaunchKernelGGL(cache_join_kernel, dim3(x.batch * x.n_kv * x.rows), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks);
   if ((e = hipGetLastError()) != hipSuccess || !x.weight) return e;
   hipLaunchKernelGGL(cache_weight_kernel, dim3((x.capacity + 255) / 256, x.n_kv, x.batch), dim3(256), 0, st, x);
   return hipGetLastError();

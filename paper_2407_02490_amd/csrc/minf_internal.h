@@ -229,9 +229,9 @@ struct CacheCall {
   int64_t q_sb, q_sh, q_st, o_sb, o_sh, o_st, k_sb, k_sh, k_st, v_sb, v_sh, v_st;
   int64_t pk_sh, pk_st, pv_sh, pv_st, w_sb, w_sh;
   int32_t batch, n_kv, group, n_new, capacity, n_init, n_local, add_weights;
-  int32_t rows, row_tiles;              // rows of a K/V head (group * n_new), in tiles of 32 or (wide) 64
+  int32_t rows, row_tiles;              // rows of a K/V head (group * n_new), in tiles of 16 row_blocks
   int32_t p_cap, p_row_tiles;           // capacity of the prefix (0: none), row tiles of its batch * rows rows
-  int32_t wide, workers, min_tiles, max_tiles, slot_rows;
+  int32_t row_blocks, workers, min_tiles, max_tiles, slot_rows;
   float c_log2;
   // workspace
   float *logits;                        // [sequence, K/V head, max_tiles][rows][32], base 2; NULL: no weights
