@@ -117,7 +117,7 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   const int64_t visible = (int64_t)x.n_init + x.n_local + x.n_new + 2 * CACHE_TILE;
   x.max_tiles = (int32_t)(((visible < x.capacity ? visible : x.capacity) + CACHE_TILE - 1) / CACHE_TILE);
   int64_t segments = (int64_t)x.batch * x.n_kv * x.row_tiles;
-  int64_t tiles = segments * x.max_tiles;
+  int64_t places = segments * (x.max_tiles + SEGMENT_COST);
   if (prefix) {
     x.pk = static_cast<const bf16_t *>(prefix->k); x.pv = static_cast<const bf16_t *>(prefix->v);
     x.p_lens = prefix->lens;
@@ -126,11 +126,10 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
     x.p_cap = prefix->capacity;
     x.p_row_tiles = (int32_t)((p_rows + tile_rows - 1) / tile_rows);
     segments += (int64_t)x.n_kv * x.p_row_tiles;
-    tiles += (int64_t)x.n_kv * x.p_row_tiles * ((prefix->capacity + CACHE_TILE - 1) / CACHE_TILE);
+    places += (int64_t)x.n_kv * x.p_row_tiles * ((prefix->capacity + CACHE_TILE - 1) / CACHE_TILE + SEGMENT_COST);
   }
-  if (tiles >= (int64_t)1 << 31) return MINF_ERR_SHAPE;                // the list of tiles is counted in 32 bits
+  if (places >= (int64_t)1 << 31) return MINF_ERR_SHAPE;               // the list of tiles is counted in 32 bits
   x.workers = CUS * 4;
-  x.min_tiles = 1;
   // workspace: O of the pieces, their maxima and sums, statistics of the rows, logits
   const size_t slots = ((size_t)2 * x.workers + (size_t)segments) * x.slot_rows;
   const size_t heads = (size_t)x.batch * x.n_kv;

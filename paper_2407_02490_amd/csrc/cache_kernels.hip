@@ -20,26 +20,40 @@ namespace minf {
 
 constexpr int CACHE_WAVES = 4;                                  // per workgroup
 constexpr int CACHE_RING = 2 * 2 * HALF_BYTES;                  // per wave: two slots of a K and a V tile
+constexpr int CACHE_LOGITS = 8192;                              // per wave: logits on their way out
 static_assert(CACHE_TILE * ROW_BYTES == HALF_BYTES, "a tile of the walk is half a 64-key tile");
 
 __device__ inline int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // ---- where a worker is in the list of tiles (wave-uniform) --------------------------------------------
-struct CacheCursor {
+// The kernel's arguments where they lie.  What a worker needs once per segment is read there, from an address
+// the compiler knows nothing about: taken from `x` it would hold all of it in scalar registers, more than there
+// are, through the tile loop.
+typedef const __attribute__((address_space(4))) CacheCall CacheArgs;
+__device__ inline CacheArgs &args_again(CacheArgs *p) {
+  asm volatile("" : "+s"(p));
+  return *p;
+}
+
+// Part of a segment (row tile of a sequence and K/V head) that a worker takes: its tiles t0 .. t1 - 1.
+struct CachePart {
   int prefix;            // 1: the shared prefix
   int b, kvh, rt;        // sequence, K/V head, row tile
-  int tau;               // tile of the segment
+  int t0, t1;
   SeqWalk w;             // of the sequence (or of the prefix)
 };
 
-__device__ inline SeqWalk walk_of(const CacheCall &x, int b) {
+template <class X>
+__device__ inline SeqWalk walk_of(X &x, int b) {
   return seq_walk(x.lens[b], x.capacity, x.n_new, x.n_init, x.n_local);
 }
-__device__ inline SeqWalk walk_of_uniform(const CacheCall &x, int b) {
+template <class X>
+__device__ inline SeqWalk walk_of_uniform(X &x, int b) {
   return seq_walk(uni(x.lens[uni(b)]), x.capacity, x.n_new, x.n_init, x.n_local);
 }
 // The prefix: every row sees all of it.
-__device__ inline SeqWalk prefix_walk(const CacheCall &x) {
+template <class X>
+__device__ inline SeqWalk prefix_walk(X &x) {
   return seq_walk(x.p_cap > 0 ? uni(x.p_lens[0]) : 0, x.p_cap, 1, 0, x.p_cap);
 }
 
@@ -52,67 +66,78 @@ __device__ inline int wave_scan(int v, int lane) {
   return v;
 }
 
-// Tiles of all sequences, per K/V head and row tile.
-__device__ inline int all_tiles(const CacheCall &x, int lane) {
+// Places of all sequences in the list, per K/V head and row tile.
+template <class X>
+__device__ inline int all_places(X &x, int lane) {
   int sum = 0;
-  for (int b0 = 0; b0 < x.batch; b0 += 64) sum += b0 + lane < x.batch ? walk_of(x, b0 + lane).tiles : 0;
+  for (int b0 = 0; b0 < x.batch; b0 += 64) sum += b0 + lane < x.batch ? walk_of(x, b0 + lane).places() : 0;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   return uni(sum);
 }
 
-// Cursor at tile g of the list; pre: tiles of the prefix.
-__device__ inline void seek(const CacheCall &x, int g, int pre, CacheCursor &c, int lane) {
+// The part that begins at place g of the list, of those before place g1 (none: t0 >= t1); pre: places of the prefix.
+template <class X>
+__device__ inline CachePart seek(X &x, int &g, int g1, int pre, int lane) {
+  CachePart c;
+  int s, at = g;
   if (g < pre) {
     c.prefix = 1;
     c.w = prefix_walk(x);
-    const int s = g / c.w.tiles;
-    c.tau = g - s * c.w.tiles;
-    c.b = 0; c.kvh = s / x.p_row_tiles; c.rt = s - c.kvh * x.p_row_tiles;
-    return;
-  }
-  g -= pre;
-  const int heads = x.n_kv * x.row_tiles;
-  int before = 0;
-  c.prefix = 0;
-  for (int b0 = 0; b0 < x.batch; b0 += 64) {
-    const int i = b0 + lane, t = i < x.batch ? walk_of(x, i).tiles : 0;
-    const int incl = wave_scan(t, lane);
-    const unsigned long long beyond = __builtin_amdgcn_ballot_w64((before + incl) * heads > g);
-    if (beyond != 0) {
-      const int at = __builtin_ctzll(beyond);
-      c.b = b0 + at;
-      before += uni(__shfl(incl, at)) - uni(__shfl(t, at));
-      break;
+    s = uni(at / c.w.places());
+    at -= s * c.w.places();
+    c.b = 0; c.kvh = uni(s / x.p_row_tiles); c.rt = s - c.kvh * x.p_row_tiles;
+  } else {
+    at -= pre;
+    const int heads = x.n_kv * x.row_tiles;
+    int before = 0;
+    c.prefix = 0;
+    c.b = 0;
+    for (int b0 = 0; b0 < x.batch; b0 += 64) {
+      const int i = b0 + lane, t = i < x.batch ? walk_of(x, i).places() : 0;
+      const int incl = wave_scan(t, lane);
+      const unsigned long long beyond = __builtin_amdgcn_ballot_w64((before + incl) * heads > at);
+      if (beyond != 0) {
+        const int first = __builtin_ctzll(beyond);
+        c.b = uni(b0 + first);
+        before += uni(__shfl(incl, first)) - uni(__shfl(t, first));
+        break;
+      }
+      before += uni(__shfl(incl, 63));
     }
-    before += uni(__shfl(incl, 63));
-  }
-  c.b = uni(c.b);
-  c.w = walk_of_uniform(x, c.b);
-  g -= before * heads;
-  const int s = g / c.w.tiles;
-  c.tau = uni(g - s * c.w.tiles);
-  c.kvh = uni(s / x.row_tiles);
-  c.rt = uni(s - c.kvh * x.row_tiles);
-}
-
-// To the next tile of the list.  False at its end.
-__device__ inline bool advance(const CacheCall &x, CacheCursor &c) {
-  if (++c.tau < c.w.tiles) return true;
-  c.tau = 0;
-  if (++c.rt < (c.prefix ? x.p_row_tiles : x.row_tiles)) return true;
-  c.rt = 0;
-  if (++c.kvh < x.n_kv) return true;
-  c.kvh = 0;
-  if (c.prefix) { c.prefix = 0; c.b = -1; }
-  for (;;) {
-    if (++c.b >= x.batch) return false;
     c.w = walk_of_uniform(x, c.b);
-    if (c.w.tiles > 0) return true;
+    at -= before * heads;
+    s = uni(at / c.w.places());
+    at -= s * c.w.places();
+    c.kvh = uni(s / x.row_tiles);
+    c.rt = s - c.kvh * x.row_tiles;
   }
+  const int head = max(SEGMENT_COST - at, 0);          // places in front of the first tile
+  g += head;
+  c.t0 = at + head - SEGMENT_COST;
+  c.t1 = min(c.w.tiles, c.t0 + g1 - g);
+  return c;
 }
 
-__device__ inline int segment_of(const CacheCall &x, const CacheCursor &c) {
+// The part behind c, of at most `most` tiles.
+template <class X>
+__device__ inline CachePart next_part(X &x, CachePart c, int most) {
+  c.t0 = 0;
+  if (++c.rt >= (c.prefix ? x.p_row_tiles : x.row_tiles)) {
+    c.rt = 0;
+    if (++c.kvh >= x.n_kv) {
+      c.kvh = 0;
+      if (c.prefix) { c.prefix = 0; c.b = -1; }
+      do c.w = walk_of_uniform(x, ++c.b);
+      while (c.w.tiles == 0);                  // there is one: the list goes on
+    }
+  }
+  c.t1 = min(c.w.tiles, most);
+  return c;
+}
+
+template <class X>
+__device__ inline int segment_of(X &x, const CachePart &c) {
   return c.prefix ? c.kvh * x.p_row_tiles + c.rt
                   : x.n_kv * x.p_row_tiles + (c.b * x.n_kv + c.kvh) * x.row_tiles + c.rt;
 }
@@ -139,7 +164,8 @@ struct CacheRows {
 struct LaneRow {
   int b, t, g;
 };
-__device__ inline LaneRow lane_row(const CacheCall &x, const CacheCursor &c, int row) {
+template <class X>
+__device__ inline LaneRow lane_row(X &x, const CachePart &c, int row) {
   LaneRow a;
   a.b = c.b;
   int r = row;
@@ -149,14 +175,14 @@ __device__ inline LaneRow lane_row(const CacheCall &x, const CacheCursor &c, int
   return a;
 }
 // This lane's row of block nb; rows behind the last one repeat it, nobody stores them.
-template <int NB>
-__device__ inline LaneRow block_row(const CacheCall &x, const CacheCursor &c, int nb, int lane) {
+template <int NB, class X>
+__device__ inline LaneRow block_row(X &x, const CachePart &c, int nb, int lane) {
   const int last = (c.prefix ? x.batch * x.rows : x.rows) - 1;
   return lane_row(x, c, min((c.rt * NB + nb) * 16 + (lane & 15), last));
 }
 
-template <int NB>
-__device__ inline void load_queries(const CacheCall &x, const CacheCursor &c, CacheQ<NB> &q, int lane) {
+template <int NB, class X>
+__device__ inline void load_queries(X &x, const CachePart &c, CacheQ<NB> &q, int lane) {
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const LaneRow a = block_row<NB>(x, c, nb, lane);
@@ -166,8 +192,8 @@ __device__ inline void load_queries(const CacheCall &x, const CacheCursor &c, Ca
   }
 }
 
-template <int NB>
-__device__ inline void begin_segment(const CacheCall &x, const CacheCursor &c, CacheRows<NB> &st, int lane) {
+template <int NB, class X>
+__device__ inline void begin_part(X &x, const CachePart &c, CacheRows<NB> &st, int lane) {
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const LaneRow a = block_row<NB>(x, c, nb, lane);
@@ -195,39 +221,70 @@ struct CacheLane {
 constexpr int HALF_TILE_ROWS = 16 * ROW_BYTES;
 __device__ inline int lane_key(int lane, int e) { return 4 * (lane >> 4) + (e & 3) + 16 * (e >> 2); }
 
+// Some value of the V tile is an infinity or NaN: the largest magnitude of its 16-bit numbers.
 __device__ inline bool tile_not_finite(const char *tV, int lane) {
+  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+  u16x8 most = 0;
+#pragma unroll
+  for (int i = 0; i < HALF_BYTES / 1024; ++i)
+    most = __builtin_elementwise_max(most, *reinterpret_cast<const u16x8 *>(tV + i * 1024 + lane * 16) & (unsigned short)0x7fff);
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < HALF_BYTES / 1024; ++i) {
-    const uint4 w = *reinterpret_cast<const uint4 *>(tV + i * 1024 + lane * 16);
-    const unsigned u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      bad = bad || (u[j] & 0x7f80u) == 0x7f80u || (u[j] & 0x7f800000u) == 0x7f800000u;
-  }
+  for (int j = 0; j < 8; ++j) bad = bad || most[j] >= 0x7f80;
   return __builtin_amdgcn_ballot_w64(bad) != 0;
 }
 
+// Logits on their way to memory (for the weights).  They wait in LDS, as they lie in memory, [tile][row][32], and
+// go out 1 KiB a store: the loop counts its loads down in order, and every store it waits for on the way costs it
+// (tiles stored one by one: 1M tokens, 8 heads of 4 rows, 963 us; without the stores 717).
+struct CacheLogits {
+  char *room;            // CACHE_LOGITS bytes of LDS
+  char *to;              // of the part's next tile in memory; rows of this row tile only
+  int tile_bytes, used, stride;     // rows x 128; bytes waiting; bytes between tiles in memory
+  __device__ inline void flush(int lane) {
+    // (tiles of several row tiles: row by row of tiles)
+    if (stride == tile_bytes) {
+      for (int i = lane * 16; i < used; i += 1024) *reinterpret_cast<uint4 *>(to + i) = *reinterpret_cast<const uint4 *>(room + i);
+    } else {
+      for (int i = lane * 16; i < used; i += 1024) {
+        const int t = i / tile_bytes;
+        *reinterpret_cast<uint4 *>(to + (int64_t)t * stride + (i - t * tile_bytes)) = *reinterpret_cast<const uint4 *>(room + i);
+      }
+    }
+    to += (int64_t)(used / tile_bytes) * stride;
+    used = 0;
+  }
+};
+
+// What the tiles of a part have in common.
+struct CacheMask {
+  int n_init, n_local, first_pos, last_pos, n_tok;
+  // every row sees every key of the tile
+  __device__ inline bool whole(int kb) const {
+    return kb + CACHE_TILE - 1 <= first_pos && (kb + CACHE_TILE - 1 < n_init || last_pos - kb < n_local);
+  }
+};
+
 // O^T += V^T P^T for the tokens one by one, with the V rows that a token does not see as zeros: 0 * inf and
 // 0 * NaN of a slot that a row's mask excludes would otherwise reach the row.  Only tiles with a mask and
-// with such values take it.  O goes through 8 KiB of LDS (`room`, the K tile that is no longer needed), so
+// with such values take it, and only where there are several tokens: slots that no row sees are not loaded.  O goes through 8 KiB of LDS (`room`, the K tile that is no longer needed), so
 // that this rare path costs the others no registers.
 template <int NB>
-__device__ inline void update_by_token(CacheRows<NB> &st, const bf16x8 (&p)[NB][2], const CacheLane &lo, const char *tV, char *room,
-                                       int kb, int n_tok, int first_pos, int n_init, int n_local, int lane) {
+__device__ inline void update_by_token(CacheRows<NB> &st, const bf16x8 (&p)[NB][2], const char *tV, char *room, int kb,
+                                       const CacheMask &mask, int lane) {
   f32x4 *mine = reinterpret_cast<f32x4 *>(room) + lane;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
     for (int db = 0; db < 8; ++db) mine[64 * db] = st.o[nb][db];
 #pragma unroll 1
-    for (int i = 0; i < 8 * n_tok; ++i) {
+    for (int i = 0; i < 8 * mask.n_tok; ++i) {
       const int db = i & 7, t = i >> 3;
       const int at = swz_byte(4 * (lane >> 4) + ((lane & 15) >> 2), 2 * db + ((lane & 3) >> 1)) + (lane & 1) * 8;
       s16x8 w = __builtin_bit_cast(s16x8, lds_read_vt(tV, at, at + HALF_TILE_ROWS));
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        w[e] = cache_visible(kb + lane_key(lane, e), first_pos + t, n_init, n_local) ? w[e] : (short)0;
+        w[e] = cache_visible(kb + lane_key(lane, e), mask.first_pos + t, mask.n_init, mask.n_local) ? w[e] : (short)0;
       const bf16x8 a = __builtin_bit_cast(bf16x8, w);
       f32x4 add = {0.f, 0.f, 0.f, 0.f};
       add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][0], add, 0, 0, 0);
@@ -244,11 +301,11 @@ __device__ inline void update_by_token(CacheRows<NB> &st, const bf16x8 (&p)[NB][
 // across lanes and no rescaling.
 constexpr float REF_ROOM = 16.f;
 
-// One tile of 32 keys.  WAIT_V: awaits the V tile (the K tile is there).
-template <int NB, class WaitV>
-__device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, CacheRows<NB> &st, const CacheLane &lo,
-                                  char *tK, const char *tV, int lane, WaitV wait_v) {
-  const int kb = c.w.base(c.tau);
+// One tile of 32 keys from slot kb on.  EDGE: some row may not see some key.  keep: the logits of the part's
+// rows_here rows are wanted.  wait_v awaits the V tile (the K tile is there).
+template <int NB, bool EDGE, class WaitV>
+__device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, const CacheLane &lo, float c_log2, int kb,
+                                  char *tK, const char *tV, bool keep, CacheLogits &out, int rows_here, int lane, WaitV wait_v) {
   f32x4 s[NB][2];
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks)
@@ -261,15 +318,12 @@ __device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, Cach
         s[nb][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, st.q.q[nb][ks], ks == 0 ? zero : s[nb][kt], 0, 0, 0);
       }
     }
-  const int n_init = c.prefix ? 0 : x.n_init, n_local = c.prefix ? x.p_cap : x.n_local;
-  const int first_pos = c.prefix ? c.w.len - 1 : c.w.i0, last_pos = c.w.len - 1, klast = kb + CACHE_TILE - 1;
-  const bool whole = klast <= first_pos && (klast < n_init || last_pos - kb < n_local);
-  if (!whole) {
+  if (EDGE) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        s[nb][e >> 2][e & 3] = cache_visible(kb + lane_key(lane, e), st.pos[nb], n_init, n_local) ? s[nb][e >> 2][e & 3] : -INFINITY;
+        s[nb][e >> 2][e & 3] = cache_visible(kb + lane_key(lane, e), st.pos[nb], mask.n_init, mask.n_local) ? s[nb][e >> 2][e & 3] : -INFINITY;
   }
   bool outgrown = false;
 #pragma unroll
@@ -277,7 +331,7 @@ __device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, Cach
     float mx = s[nb][0][0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[nb][e >> 2][e & 3]);
-    outgrown = outgrown || mx * x.c_log2 > st.m[nb] + REF_ROOM;
+    outgrown = outgrown || mx * c_log2 > st.m[nb] + REF_ROOM;
   }
   if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
 #pragma unroll
@@ -286,7 +340,7 @@ __device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, Cach
 #pragma unroll
       for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[nb][e >> 2][e & 3]);
       mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * x.c_log2;
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) * c_log2;
       const float m_new = fmaxf(st.m[nb], mx);
       const float f = m_new == -INFINITY ? 1.f : fast_exp2(st.m[nb] - m_new);
       st.m[nb] = m_new;
@@ -304,7 +358,7 @@ __device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, Cach
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
-      const f32x2 v = {fast_exp2(fmaf(s[nb][e >> 2][e & 3], x.c_log2, -m)), fast_exp2(fmaf(s[nb][e >> 2][(e & 3) + 1], x.c_log2, -m))};
+      const f32x2 v = {fast_exp2(fmaf(s[nb][e >> 2][e & 3], c_log2, -m)), fast_exp2(fmaf(s[nb][e >> 2][(e & 3) + 1], c_log2, -m))};
       sum += v[0] + v[1];
       const bf16x2 hi = __builtin_convertvector(v, bf16x2);
       const f32x2 rest = {v[0] - (float)hi[0], v[1] - (float)hi[1]};
@@ -315,8 +369,8 @@ __device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, Cach
     st.l[nb] += sum;
   }
   wait_v();
-  if (!whole && tile_not_finite(tV, lane)) {
-    update_by_token<NB>(st, p, lo, tV, tK, kb, c.prefix ? 1 : x.n_new, first_pos, n_init, n_local, lane);
+  if (EDGE && mask.n_tok > 1 && tile_not_finite(tV, lane)) {
+    update_by_token<NB>(st, p, tV, tK, kb, mask, lane);
   } else {
 #pragma unroll
     for (int db = 0; db < 8; ++db) {
@@ -328,23 +382,28 @@ __device__ inline void cache_tile(const CacheCall &x, const CacheCursor &c, Cach
           st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][part], st.o[nb][db], 0, 0, 0);
     }
   }
-  if (x.logits && !c.prefix) {
-    float *row0 = x.logits + (((int64_t)c.b * x.n_kv + c.kvh) * x.max_tiles + c.tau) * (x.rows * CACHE_TILE) + 4 * (lane >> 4);
+  if (keep) {
+    const int row = lane & 15;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const int row = (c.rt * NB + nb) * 16 + (lane & 15);
-      if (row < x.rows) {
+    for (int nb = 0; nb < NB; ++nb)
+      if (16 * nb + row < rows_here) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) *reinterpret_cast<f32x4 *>(row0 + row * CACHE_TILE + 16 * kt) = s[nb][kt] * x.c_log2;
+        for (int kt = 0; kt < 2; ++kt)
+          *reinterpret_cast<f32x4 *>(out.room + out.used + (16 * nb + row) * 128 + 64 * kt + 16 * (lane >> 4)) = s[nb][kt] * c_log2;
       }
+    out.used += out.tile_bytes;
+    if (out.used + out.tile_bytes > CACHE_LOGITS) {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      out.flush(lane);
     }
   }
 }
 
 // End of a worker's part of a segment: rows of O that are final go out, others into the workspace.
-template <int NB>
-__device__ inline void end_segment(const CacheCall &x, const CacheCursor &c, const CacheRows<NB> &st, bool whole,
-                                   int slot, int lane) {
+template <int NB, class X>
+__device__ inline void end_part(X &x, const CachePart &c, const CacheRows<NB> &st, bool whole, int slot, int lane) {
   const int n = lane & 15, g = lane >> 4, rows = c.prefix ? x.batch * x.rows : x.rows;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
@@ -388,99 +447,161 @@ struct CacheSource {
 #pragma unroll
     for (unsigned j = 0; j < 4; ++j) ofs[j] = (4 * j + rl) * rb + (((cpos ^ (rl << 2)) ^ j) << 4) - 1024 * j;
   }
-  __device__ inline void strides(const CacheCall &x, int prefix, int lane) {
+  template <class X>
+  __device__ inline void strides(X &x, int prefix, int lane) {
     k_rb = (unsigned)(prefix ? x.pk_st : x.k_st) * 2u;
     v_rb = (unsigned)(prefix ? x.pv_st : x.v_st) * 2u;
     lanes(kofs, k_rb, lane);
     lanes(vofs, v_rb, lane);
   }
-  __device__ inline void heads(const CacheCall &x, const CacheCursor &c) {
+  template <class X>
+  __device__ inline void heads(X &x, const CachePart &c) {
     kh = reinterpret_cast<const char *>(c.prefix ? x.pk + c.kvh * x.pk_sh : x.k + c.b * x.k_sb + c.kvh * x.k_sh);
     vh = reinterpret_cast<const char *>(c.prefix ? x.pv + c.kvh * x.pv_sh : x.v + c.b * x.v_sb + c.kvh * x.v_sh);
   }
-  // 32 rows from kb on into the tile at lds; rows behind the last token repeat it (masked, and in bounds)
-  __device__ static inline void tile(const char *h, unsigned rb, const unsigned (&ofs)[4], int kb, int len, unsigned lds, int lane) {
-    if (kb + CACHE_TILE <= len) {
+  // 32 rows from kb on into the tile at lds
+  __device__ static inline void tile(const char *h, unsigned rb, const unsigned (&ofs)[4], int kb, unsigned lds) {
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const char *row0 = h + (uint64_t)(unsigned)(kb + 16 * half) * rb;
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\t"
-                     "global_load_lds_dwordx4 %0, %1\n\t"
-                     "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
-                     "global_load_lds_dwordx4 %5, %1 offset:3072"
-                     :: "v"(ofs[0]), "s"(row0), "s"(lds + 4096 * half), "v"(ofs[1]), "v"(ofs[2]), "v"(ofs[3]) : "memory");
-      }
-      return;
+    for (int half = 0; half < 2; ++half) {
+      const char *row0 = h + (uint64_t)(unsigned)(kb + 16 * half) * rb;
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                   "global_load_lds_dwordx4 %0, %1\n\t"
+                   "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                   "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
+                   "global_load_lds_dwordx4 %5, %1 offset:3072"
+                   :: "v"(ofs[0]), "s"(row0), "s"(lds + 4096 * half), "v"(ofs[1]), "v"(ofs[2]), "v"(ofs[3]) : "memory");
     }
+  }
+  // ... row by row: slots that no row of the call sees are replaced by one that some row does
+  __device__ static inline void tile_in_part(const char *h, unsigned rb, int kb, const SeqWalk &w, unsigned lds, int lane) {
     const int rl = lane >> 4, cpos = lane & 15;
 #pragma unroll
     for (int blk = 0; blk < 8; ++blk) {
       const int r = 4 * blk + rl;
-      dma16(h + (uint64_t)(unsigned)min(kb + r, len - 1) * rb + ((cpos ^ swz_f(r)) << 4), lds + blk * 1024);
+      int key = kb + r;
+      if (key >= w.e1) key = max(key, w.lo);
+      key = min(key, w.len - 1);
+      dma16(h + (uint64_t)(unsigned)key * rb + ((cpos ^ swz_f(r)) << 4), lds + blk * 1024);
     }
   }
-  __device__ inline void fetch(int kb, int len, unsigned lds, int lane) const {
-    tile(kh, k_rb, kofs, kb, len, lds, lane);
-    tile(vh, v_rb, vofs, kb, len, lds + HALF_BYTES, lane);
+  __device__ inline void fetch(int kb, const SeqWalk &w, unsigned lds, int lane) const {
+    const int end = kb + CACHE_TILE;
+    if (end <= w.len && (kb >= w.lo || end <= w.e1)) {
+      tile(kh, k_rb, kofs, kb, lds);
+      tile(vh, v_rb, vofs, kb, lds + HALF_BYTES);
+    } else {
+      tile_in_part(kh, k_rb, kb, w, lds, lane);
+      tile_in_part(vh, v_rb, kb, w, lds + HALF_BYTES, lane);
+    }
   }
 };
 
+// Two waves per SIMD fit (256 registers): with more to hand out the compiler moves O between register files
+// in every tile.
 template <int NB>
-__global__ __launch_bounds__(64 * CACHE_WAVES) void cache_attn_kernel(CacheCall x) {
+__global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_kernel(CacheCall) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
+  CacheArgs *args = (CacheArgs *)__builtin_amdgcn_kernarg_segment_ptr();
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   const int worker = blockIdx.x * CACHE_WAVES + wave;
   char *ring = lds + wave * CACHE_RING;
   const unsigned ring_at = uni(lds_addr_of(ring));
 
-  const int pre = prefix_walk(x).tiles * x.n_kv * x.p_row_tiles;
-  const int total = pre + all_tiles(x, lane) * x.n_kv * x.row_tiles;
-  const int share = worker_share(total, x.workers, x.min_tiles);
-  const int g0 = worker * share, g1 = min(g0 + share, total);
-  if (g0 >= g1) return;
-
-  CacheCursor cur, nxt;
-  seek(x, g0, pre, cur, lane);
+  int first_place, g, g1;                    // place of the current part's first tile, end of this worker's places
+  CachePart cur;
+  {
+    CacheArgs &x = args_again(args);
+    const int pre = prefix_walk(x).places() * x.n_kv * x.p_row_tiles;
+    const int total = pre + all_places(x, lane) * x.n_kv * x.row_tiles;
+    const int share = worker_share(total, x.workers);
+    first_place = g = worker * share;
+    g1 = min(g + share, total);
+    if (g >= g1) return;
+    cur = seek(x, g, g1, pre, lane);
+    if (cur.t0 >= cur.t1) return;
+  }
   CacheSource src;
-  src.strides(x, cur.prefix, lane);
-  src.heads(x, cur);
   CacheRows<NB> st;
-  CacheQ<NB> q;                              // rows of the next segment, loaded ahead of its first tile (loads return in order)
-  load_queries<NB>(x, cur, st.q, lane);
-  src.fetch(cur.w.base(cur.tau), cur.w.len, ring_at, lane);
+  CacheQ<NB> q;                              // rows of the next part, loaded ahead of its first tile (loads return in order)
+  {
+    CacheArgs &x = args_again(args);
+    src.strides(x, cur.prefix, lane);
+    src.heads(x, cur);
+    load_queries<NB>(x, cur, st.q, lane);
+  }
+  src.fetch(cur.w.base(cur.t0), cur.w, ring_at, lane);
   CacheLane lo;
   lo.init(lane);
-  int piece_t0 = cur.tau;                    // first tile of this worker's part of the segment
-  begin_segment<NB>(x, cur, st, lane);
-  for (int g = g0, slot = 0;; ++g, slot ^= 1) {
-    nxt = cur;
-    const bool more = g + 1 < g1 && advance(x, nxt);
-    if (more) {
-      if (nxt.tau == 0) {                    // the next segment's rows, ahead of its first tile
+  const float c_log2 = args->c_log2;
+  unsigned slot = 0;
+  // The compiler waits for the rows where they are used first.  Here, once: inside the loop it would wait for all
+  // loads in every iteration, the tiles' too.
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(st.q.q[nb][ks]));
+  CacheLogits out;
+  out.room = lds + CACHE_WAVES * CACHE_RING + wave * CACHE_LOGITS;
+  out.used = 0;
+  for (;;) {                                 // part by part
+    const int left = g1 - g - (cur.t1 - cur.t0) - SEGMENT_COST;        // tiles of the next one at most
+    CachePart nxt;
+    CacheMask mask;
+    int rows_here;
+    bool keep;
+    {
+      CacheArgs &x = args_again(args);
+      if (left > 0) nxt = next_part(x, cur, left);
+      begin_part<NB>(x, cur, st, lane);
+      mask.n_init = cur.prefix ? 0 : x.n_init;
+      mask.n_local = cur.prefix ? x.p_cap : x.n_local;
+      mask.first_pos = cur.prefix ? cur.w.len - 1 : cur.w.i0;
+      mask.last_pos = cur.w.len - 1;
+      mask.n_tok = cur.prefix ? 1 : x.n_new;
+      rows_here = min(x.rows - cur.rt * NB * 16, NB * 16);
+      keep = x.logits && !cur.prefix;
+      out.tile_bytes = rows_here * CACHE_TILE * 4;
+      out.stride = x.rows * CACHE_TILE * 4;
+      out.to = reinterpret_cast<char *>(x.logits) +
+               ((((int64_t)cur.b * x.n_kv + cur.kvh) * x.max_tiles + cur.t0) * x.rows + cur.rt * NB * 16) * (CACHE_TILE * 4);
+    }
+    for (int t = cur.t0, kb = cur.w.base(t); t < cur.t1; ++t) {
+      const int kb_next = t + 1 == cur.w.T1 ? cur.w.s2 : kb + CACHE_TILE;
+      const bool more = t + 1 < cur.t1 || left > 0;
+      if (t + 1 < cur.t1) {
+        src.fetch(kb_next, cur.w, ring_at + (slot ^ 2 * HALF_BYTES), lane);
+      } else if (left > 0) {
+        CacheArgs &x = args_again(args);
         if (nxt.prefix != cur.prefix) src.strides(x, nxt.prefix, lane);
         src.heads(x, nxt);
         load_queries<NB>(x, nxt, q, lane);
+        src.fetch(nxt.w.base(0), nxt.w, ring_at + (slot ^ 2 * HALF_BYTES), lane);
       }
-      src.fetch(nxt.w.base(nxt.tau), nxt.w.len, ring_at + (slot ^ 1) * (2 * HALF_BYTES), lane);
-      MINF_WAIT_VMCNT(24);                   // of the tile before: K has landed
-    } else {
-      MINF_WAIT_VMCNT(8);
+      if (more) MINF_WAIT_VMCNT(24); else MINF_WAIT_VMCNT(8);     // K has landed
+      auto wait_v = [&]() {
+        if (more) MINF_WAIT_VMCNT(16); else MINF_WAIT_VMCNT(0);
+      };
+      char *tK = ring + slot;
+      if (mask.whole(kb)) cache_tile<NB, false>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, rows_here, lane, wait_v);
+      else cache_tile<NB, true>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, rows_here, lane, wait_v);
+      __builtin_amdgcn_s_waitcnt(0xC07F);    // LDS reads done: the slot may be filled again
+      slot ^= 2 * HALF_BYTES;
+      kb = kb_next;
     }
-    char *tK = ring + slot * 2 * HALF_BYTES;
-    cache_tile<NB>(x, cur, st, lo, tK, tK + HALF_BYTES, lane, [&]() {
-      if (more) MINF_WAIT_VMCNT(16); else MINF_WAIT_VMCNT(0);
-    });
-    __builtin_amdgcn_s_waitcnt(0xC07F);      // LDS reads done: the slot may be filled again
-    if (!more || nxt.tau == 0) {
-      const bool whole = piece_t0 == 0 && cur.tau == cur.w.tiles - 1;
-      const int first_g = g - (cur.tau - piece_t0);
-      end_segment<NB>(x, cur, st, whole, whole ? 2 * x.workers + segment_of(x, cur) : 2 * worker + (first_g > g0 ? 1 : 0), lane);
-      if (!more) break;
-      st.q = q;
-      begin_segment<NB>(x, nxt, st, lane);
-      piece_t0 = 0;
+    {
+      CacheArgs &x = args_again(args);
+      if (keep) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        out.flush(lane);
+      }
+      const bool whole = cur.t0 == 0 && cur.t1 == cur.w.tiles;
+      end_part<NB>(x, cur, st, whole, whole ? 2 * x.workers + segment_of(x, cur) : 2 * worker + (g > first_place ? 1 : 0), lane);
     }
+    if (left <= 0) break;
+    g += cur.t1 - cur.t0 + SEGMENT_COST;
+    st.q = q;
     cur = nxt;
   }
 }
@@ -495,11 +616,12 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   const int row = blockIdx.x % x.rows, seg = blockIdx.x / x.rows;      // of the sequence and K/V head
   const int b = seg / x.n_kv, kvh = seg - b * x.n_kv;
-  const int pt = prefix_walk(x).tiles, pre = pt * x.n_kv * x.p_row_tiles;
+  const SeqWalk pw = prefix_walk(x);
+  const int pre = pw.places() * x.n_kv * x.p_row_tiles;
   const int heads = x.n_kv * x.row_tiles;
   int before = 0, all = 0;
   for (int b0 = 0; b0 < x.batch; b0 += 64) {
-    const int i = b0 + lane, t = i < x.batch ? walk_of(x, i).tiles : 0;
+    const int i = b0 + lane, t = i < x.batch ? walk_of(x, i).places() : 0;
     all += t;
     before += i < b ? t : 0;
   }
@@ -508,11 +630,11 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
     all += __shfl_xor(all, d);
     before += __shfl_xor(before, d);
   }
-  const int share = worker_share(uni(pre + all * heads), x.workers, x.min_tiles);
+  const int share = worker_share(uni(pre + all * heads), x.workers);
   const SeqWalk w = walk_of_uniform(x, b);
   const int t = row / x.group, rt = row / tile_rows;
   const bool token = w.i0 + t >= 0;
-  const int own0 = uni(pre + before * heads + (kvh * x.row_tiles + rt) * w.tiles);
+  const int own0 = uni(pre + before * heads + (kvh * x.row_tiles + rt) * w.places() + SEGMENT_COST);
   if (x.p_cap == 0 && w.tiles > 0) {
     const SegmentPieces p = segment_pieces(own0, own0 + w.tiles, share);
     if (p.first == p.last) return;                                     // written by the worker itself
@@ -565,7 +687,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
     join(own0, w.tiles, row - rt * tile_rows, x.n_kv * x.p_row_tiles + (b * x.n_kv + kvh) * x.row_tiles + rt);
     if (x.p_cap > 0) {
       const int prow = b * x.rows + row, prt = prow / tile_rows;
-      join((kvh * x.p_row_tiles + prt) * pt, pt, prow - prt * tile_rows, kvh * x.p_row_tiles + prt);
+      join((kvh * x.p_row_tiles + prt) * pw.places() + SEGMENT_COST, pw.tiles, prow - prt * tile_rows, kvh * x.p_row_tiles + prt);
     }
   }
   __shared__ float sm[JOIN_WAVES], sl[JOIN_WAVES];
@@ -593,26 +715,30 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   if (x.stat && lane == 0) x.stat[(int64_t)seg * x.rows + row] = float2{m, inv};
 }
 
-// Weight of every slot: the column sums of the softmax, from the logits that the workers left.
+// Weight of every slot: the column sums of the softmax, from the logits that the workers left.  A thread takes
+// four slots of a tile (slots and tiles are aligned alike).
 __global__ __launch_bounds__(256) void cache_weight_kernel(CacheCall x) {
-  const int slot = blockIdx.x * 256 + threadIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+  const int slot = 4 * (blockIdx.x * 256 + threadIdx.x), kvh = blockIdx.y, b = blockIdx.z;
   const SeqWalk w = walk_of_uniform(x, b);
   if (slot >= w.len) return;
   const int tau = w.tile_of(slot);
-  float sum = 0.f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   if (tau >= 0) {
     const int64_t head = (int64_t)b * x.n_kv + kvh;
     const float *s = x.logits + (head * x.max_tiles + tau) * (x.rows * CACHE_TILE) + (slot - w.base(tau));
     const float2 *st = x.stat + head * x.rows;
-#pragma unroll 8
+#pragma unroll 4
     for (int r = 0; r < x.rows; ++r) {
-      const float v = s[r * CACHE_TILE];
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(s + r * CACHE_TILE);
       const float2 ml = st[r];
-      sum += v == -INFINITY ? 0.f : fast_exp2(v - ml.x) * ml.y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += v[i] == -INFINITY ? 0.f : fast_exp2(v[i] - ml.x) * ml.y;
     }
   }
   float *to = x.weight + b * x.w_sb + kvh * x.w_sh + slot;
-  *to = x.add_weights ? *to + sum : sum;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (slot + i < w.len) to[i] = x.add_weights ? to[i] + sum[i] : sum[i];
 }
 
 // ---- eviction ---------------------------------------------------------------------------------------------
@@ -901,7 +1027,7 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictCall x, int in_pla
 // ---- host-side launches -------------------------------------------------------------------------------------
 template <int NB>
 static hipError_t launch_workers(const CacheCall &x, hipStream_t st) {
-  const size_t lds = CACHE_WAVES * CACHE_RING;
+  const size_t lds = CACHE_WAVES * (CACHE_RING + (x.logits ? CACHE_LOGITS : 0));
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_attn_kernel<NB>),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
@@ -914,7 +1040,7 @@ hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(cache_join_kernel, dim3(x.batch * x.n_kv * x.rows), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks);
   if ((e = hipGetLastError()) != hipSuccess || !x.weight) return e;
-  hipLaunchKernelGGL(cache_weight_kernel, dim3((x.capacity + 255) / 256, x.n_kv, x.batch), dim3(256), 0, st, x);
+  hipLaunchKernelGGL(cache_weight_kernel, dim3((x.capacity + 1023) / 1024, x.n_kv, x.batch), dim3(256), 0, st, x);
   return hipGetLastError();
 }
 

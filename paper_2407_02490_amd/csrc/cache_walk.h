@@ -18,11 +18,16 @@
 namespace minf {
 
 constexpr int CACHE_TILE = 32;
+// A segment (below) costs a worker its tiles and, for its rows and its result, as much as two more: it takes up so
+// many places more in the list, in front of its tiles.
+constexpr int SEGMENT_COST = 2;
 
 // Tiles of one sequence: T1 tiles of the sink from slot 0 on, then the window's from slot s2 (a multiple of
 // the tile) on.  Sink and window that touch in a tile are walked as one (T1 = 0, s2 = 0).
 struct SeqWalk {
   int32_t len, i0, T1, s2, tiles;       // i0: position of the first of the n_new rows (negative: no token)
+  int32_t e1, lo;                       // some row sees the slots 0 .. e1 - 1 and lo .. len - 1, no row another one
+  MINF_HD int32_t places() const { return tiles > 0 ? tiles + SEGMENT_COST : 0; }
   MINF_HD int32_t base(int32_t t) const { return t < T1 ? t * CACHE_TILE : s2 + (t - T1) * CACHE_TILE; }
   // tile that holds a slot, or -1
   MINF_HD int32_t tile_of(int32_t slot) const {
@@ -36,10 +41,11 @@ MINF_HD SeqWalk seq_walk(int32_t len, int32_t capacity, int32_t n_new, int32_t n
   SeqWalk w;
   w.len = len < 0 ? 0 : (len > capacity ? capacity : len);
   w.i0 = w.len - n_new;
-  const int32_t e1 = n_init < w.len ? n_init : w.len;
-  const int32_t lo = w.i0 - n_local + 1;
-  w.s2 = lo > 0 ? lo / CACHE_TILE * CACHE_TILE : 0;
-  w.T1 = (e1 + CACHE_TILE - 1) / CACHE_TILE;
+  w.e1 = n_init < w.len ? n_init : w.len;
+  w.lo = w.i0 - n_local + 1;
+  if (w.lo < 0) w.lo = 0;
+  w.s2 = w.lo / CACHE_TILE * CACHE_TILE;
+  w.T1 = (w.e1 + CACHE_TILE - 1) / CACHE_TILE;
   if (w.s2 <= w.T1 * CACHE_TILE) w.s2 = w.T1 = 0;
   w.tiles = w.T1 + (w.len - w.s2 + CACHE_TILE - 1) / CACHE_TILE;
   return w;
@@ -49,14 +55,14 @@ MINF_HD bool cache_visible(int32_t key, int32_t pos, int32_t n_init, int32_t n_l
   return key <= pos && (key < n_init || pos - key < n_local);
 }
 
-// Tiles per worker: equal shares, but at least min_tiles.
-MINF_HD int32_t worker_share(int32_t total, int32_t workers, int32_t min_tiles) {
+// Places per worker: equal shares.
+MINF_HD int32_t worker_share(int32_t total, int32_t workers) {
   const int32_t c = (total + workers - 1) / workers;
-  return c < min_tiles ? min_tiles : c;
+  return c < 1 ? 1 : c;
 }
 
-// Workers of the segment (one row tile of one sequence and K/V head) that holds the tiles [t0, t1) of the
-// list: first .. last.  The part that begins at a worker's own first tile is its piece 0, another one its
+// Workers of the segment (one row tile of one sequence and K/V head) whose tiles lie at the places [t0, t1) of
+// the list: first .. last.  The part that begins at a worker's own first place is its piece 0, another one its
 // piece 1: no worker has more than two parts of segments that it does not hold whole.
 struct SegmentPieces {
   int32_t first, last;

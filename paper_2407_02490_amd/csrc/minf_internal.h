@@ -231,7 +231,7 @@ struct CacheCall {
   int32_t batch, n_kv, group, n_new, capacity, n_init, n_local, add_weights;
   int32_t rows, row_tiles;              // rows of a K/V head (group * n_new), in tiles of 16 row_blocks
   int32_t p_cap, p_row_tiles;           // capacity of the prefix (0: none), row tiles of its batch * rows rows
-  int32_t row_blocks, workers, min_tiles, max_tiles, slot_rows;
+  int32_t row_blocks, workers, max_tiles, slot_rows;
   float c_log2;
   // workspace
   float *logits;                        // [sequence, K/V head, max_tiles][rows][32], base 2; NULL: no weights

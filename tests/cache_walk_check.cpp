@@ -46,6 +46,8 @@ static int walks() {
               for (int t = 0; t < T; ++t) seen = seen || (w.i0 + t >= 0 && cache_visible(j, w.i0 + t, ni, nl));
               CHECK(times[j] <= 1);
               CHECK(!seen || times[j] == 1);
+              CHECK(!seen || j < w.e1 || j >= w.lo);
+              CHECK(T > 1 || seen == (j < w.e1 || j >= w.lo));
               CHECK((w.tile_of(j) >= 0) == (times[j] == 1));
             }
           }
@@ -57,17 +59,17 @@ static int shares() {
   int cases = 0;
   const std::vector<std::vector<int>> lists = {{1}, {5, 0, 3}, {40, 1, 1, 1, 300, 2}, {0, 0}, {7, 7, 7, 7, 7, 7, 7}, {5000}};
   for (const auto &tiles : lists)
-    for (int workers : {1, 4, 64, 1024})
-      for (int least : {1, 2, 8}) {
+    for (int workers : {1, 4, 64, 1024}) {
         ++cases;
         int total = 0;
-        for (int t : tiles) total += t;
-        const int share = worker_share(total, workers, least);
+        for (int t : tiles) total += t > 0 ? t + SEGMENT_COST : 0;
+        const int share = worker_share(total, workers);
         CHECK((int64_t)share * workers >= total);
         std::set<int> used;
         int t0 = 0;
         for (int t : tiles) {
           if (t == 0) continue;
+          t0 += SEGMENT_COST;
           const SegmentPieces p = segment_pieces(t0, t0 + t, share);
           CHECK(p.first >= 0 && p.last < workers && p.first <= p.last);
           if (p.first != p.last) {
