@@ -57,6 +57,7 @@
 #include <string.h>
 #include <type_traits>
 
+#include "cache_walk.h"
 #include "dispatch.h"
 #include "mfma_tile.h"
 #include "vs_ring_sched.h"
@@ -675,8 +676,9 @@ __device__ inline void qk_tile_v(f32x16 (&s)[2][2], const QAcc &qa, const LaneOf
         mfma_qk_acc(s[mb][1], a, qa.q[1][ks]);
       }
     }
-  // the vector ALU may read s 18 wait states after the last MFMA was issued
-  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
+  // the vector ALU may read s 18 wait states after the last MFMA was issued; s passes through here, so that no
+  // reader of it is moved in front (where no branch lies between, the row maximum was)
+  asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]) :: "memory");
 }
 
 // Per-lane offsets of the pipelines' tile loads, for any distance between rows.  The four 1 KiB blocks
@@ -2912,10 +2914,112 @@ __global__ __launch_bounds__(256) void vs_ring_kernel(QKV x, HeadList hl, const 
 }
 
 // ---------------------------------------------------------------------------
+// Cache calls with many rows per K/V head (a prefix shared by a batch, many new tokens): the slots that every row
+// sees, in whole 64-key tiles.  256 rows share the tiles as in ashape_kernel, without a mask; a workgroup takes
+// one part of the slots of one row tile and leaves its references, sums and unnormalised O in the workspace for
+// cache_join_kernel.  From 33 rows on: the workers of cache_kernels.hip read the slots once per 32 rows, this
+// kernel once per 256, at 1.3 PFLOP/s with all of them in use.
+// Launch order: the row tiles that read the same slots run on one XCD, one after the other.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int per_xcd = blockIdx.x >> 3, rt = per_xcd % x.c_row_tiles;
+  const int group = (per_xcd / x.c_row_tiles) * 8 + (blockIdx.x & 7);        // (K/V head of a sequence, part of the slots)
+  const int heads = (x.p_common ? 1 : x.batch) * x.n_kv;
+  if (group >= heads * x.c_splits) return;
+  const int head = group / x.c_splits, part = group - head * x.c_splits;
+  const int b = x.p_common ? 0 : head / x.n_kv, kvh = head - b * x.n_kv;
+  const int len = x.p_common ? x.p_lens[0] : x.lens[b], cap = x.p_common ? x.p_cap : x.capacity;
+  const int tiles = to_sgpr(common_slots((len < 0 ? 0 : min(len, cap)) - (x.p_common ? 1 : x.n_new)) / COMMON_TILE);
+  const int per = common_share(tiles, x.c_splits), t0 = to_sgpr(part * per), n = to_sgpr(min(per, tiles - t0));
+  if (n <= 0) return;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  AshapeCtx c;
+  c.k_st = x.p_common ? x.pk_st : x.k_st; c.v_st = x.p_common ? x.pv_st : x.v_st;
+  c.kh = (x.p_common ? x.pk + kvh * x.pk_sh : x.k + b * x.k_sb + kvh * x.k_sh) + (int64_t)t0 * COMMON_TILE * c.k_st;
+  c.vh = (x.p_common ? x.pv + kvh * x.pv_sh : x.v + b * x.v_sb + kvh * x.v_sh) + (int64_t)t0 * COMMON_TILE * c.v_st;
+  c.N = n * COMMON_TILE; c.T1 = 0; c.T = n; c.s2 = 0; c.lds = lds; c.c_log2 = x.c_log2;
+  WaveDma d;
+  d.k_rb = (unsigned)c.k_st * 2u; d.v_rb = (unsigned)c.v_st * 2u;
+  d.k.init(d.k_rb, lane);
+  d.v.init(d.v_rb, lane);
+  d.kw = reinterpret_cast<const char *>(c.kh) + (size_t)(16 * wave) * d.k_rb;
+  d.vw = reinterpret_cast<const char *>(c.vh) + (size_t)(16 * wave) * d.v_rb;
+  d.lds_w = wave * 4096;
+  ashape_first_loads(c, d);
+
+  WaveState st;
+  auto load_rows = [&]() {
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb) {
+      int row = min(rt * 256 + wave * 64 + 32 * nb + (lane & 31), x.c_rows - 1);   // rows behind the last repeat it
+      int rb = b;
+      if (x.p_common) { rb = row / x.rows; row -= rb * x.rows; }
+      const int t = row / x.group;
+      const bf16_t *q = x.q + rb * x.q_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.q_sh + t * x.q_st + 8 * (lane >> 5);
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) st.q[nb][ks] = *reinterpret_cast<const bf16x8 *>(q + 16 * ks);
+    }
+  };
+  load_rows();
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb) {
+    set_reference(st, nb, 0.f);
+    st.l[nb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[db][nb][r] = 0.f;
+  }
+  LaneOfs lo;
+  lane_offsets(lo, lane);
+  MaskP mp;                                // every key of the part, for the rows of all waves
+  mp.q0 = 1 << 30; mp.lo = 0; mp.hi = 1 << 30; mp.n_init = 0; mp.n_local = (1 << 30) + BQ;
+  QAcc qa;
+  pin_q(qa, st);
+  bool has_ref = false;
+  ashape_pass_pipelined<AllCls>(c, d, st, qa, has_ref, lo, mp, AllCls(), lane);
+  if (__syncthreads_or(needs_exact(st) ? 1 : 0)) {
+    load_rows();
+    reset_for_max_pass(st);
+    ashape_pass<PASS_MAX>(c, st, lo, mp, wave, lane);
+    finish_max_pass(st, x.c_log2);
+    ashape_pass<PASS_FIX>(c, st, lo, mp, wave, lane);
+  }
+  const int64_t item = ((int64_t)head * x.c_row_tiles + rt) * x.c_splits + part;
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb) {
+    const int in_tile = wave * 64 + 32 * nb + (lane & 31), h = lane >> 5;
+    const float l = st.l[nb] + __shfl_xor(st.l[nb], 32);
+    if (rt * 256 + in_tile >= x.c_rows) continue;
+    const int64_t at = item * 256 + in_tile;
+    if (h == 0) x.common_ml[at] = float2{st.m[nb], l};
+    float *to = x.common_o + at * D + 4 * h;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4 *>(to + 32 * db + 8 * g) = float4{st.o[db][nb][4 * g], st.o[db][nb][4 * g + 1],
+                                                                   st.o[db][nb][4 * g + 2], st.o[db][nb][4 * g + 3]};
+  }
+}
+
+// ---------------------------------------------------------------------------
 // host-side launches
 // ---------------------------------------------------------------------------
 static hipError_t set_lds(const void *fn, size_t bytes) {
   return hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+hipError_t launch_cache_common(const CacheCall &x, hipStream_t st) {
+  const size_t lds = 8 * TILE_BYTES;
+  hipError_t e = set_lds(reinterpret_cast<const void *>(cache_common_kernel), lds);
+  if (e != hipSuccess) return e;
+  const int groups = (x.p_common ? 1 : x.batch) * x.n_kv * x.c_splits;
+  hipLaunchKernelGGL(cache_common_kernel, dim3((groups + 7) / 8 * 8 * x.c_row_tiles), dim3(256), lds, st, x);
+  return hipGetLastError();
 }
 
 hipError_t launch_ashape(const QKV &x, int nb, const HeadList &hl, int n_init, int n_local, hipStream_t st) {

@@ -77,8 +77,20 @@ minf_status check_queries(const minf_queries *x, const minf_kv_cache *c, bool ne
 // Everything but the workspace's addresses; need: its bytes.
 struct Plan {
   CacheCall x;
-  size_t need, at_ml, at_stat, at_logits;
+  size_t need, at_ml, at_common, at_common_ml, at_stat, at_logits;
 };
+
+// Parts that the common slots of `items` row tiles are cut into: as many workgroups, one per CU, in rounds.  A
+// workgroup's start and end cost about as much as six tiles.
+int common_splits(int64_t items, int64_t tiles) {
+  int best = 1;
+  int64_t least = INT64_MAX;
+  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    const int64_t time = (items * s + CUS - 1) / CUS * (common_share((int32_t)tiles, s) + 6);
+    if (time < least) { least = time; best = s; }
+  }
+  return best;
+}
 
 minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_kv_cache *prefix, int32_t n_init,
                       int32_t n_local, int32_t weights, bool need_o, Plan &p) {
@@ -113,6 +125,10 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   const int tile_rows = 16 * x.row_blocks;
   x.row_tiles = (x.rows + tile_rows - 1) / tile_rows;
   x.slot_rows = prefix || x.rows > tile_rows ? tile_rows : x.rows;
+  const bool whole_cache = x.n_local == x.capacity;
+  x.p_common = prefix && p_rows > 32 && prefix->capacity >= COMMON_TILE;
+  x.own_common = !prefix && x.rows > 32 && whole_cache && x.capacity >= 2 * COMMON_TILE;
+  x.direct = !prefix && !x.own_common;
   // the longest walk: sink and window, each with a tile that it fills in part
   const int64_t visible = (int64_t)x.n_init + x.n_local + x.n_new + 2 * CACHE_TILE;
   x.max_tiles = (int32_t)(((visible < x.capacity ? visible : x.capacity) + CACHE_TILE - 1) / CACHE_TILE);
@@ -130,19 +146,31 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   }
   if (places >= (int64_t)1 << 31) return MINF_ERR_SHAPE;               // the list of tiles is counted in 32 bits
   x.workers = CUS * 4;
-  // workspace: O of the pieces, their maxima and sums, statistics of the rows, logits
+  // workspace: O of the pieces, their maxima and sums, the same of the common slots' parts, statistics of the
+  // rows, logits (for the weights of up to 16 rows)
   const size_t slots = ((size_t)2 * x.workers + (size_t)segments) * x.slot_rows;
   const size_t heads = (size_t)x.batch * x.n_kv;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   p.at_ml = up(slots * 128 * sizeof(float));
-  p.at_stat = p.at_ml + up(slots * sizeof(float2));
+  p.at_common = p.at_common_ml = p.at_stat = p.at_ml + up(slots * sizeof(float2));
+  if (x.p_common || x.own_common) {
+    x.c_rows = (int32_t)(prefix ? p_rows : x.rows);
+    x.c_row_tiles = (x.c_rows + 255) / 256;
+    const int64_t items = (int64_t)(prefix ? 1 : x.batch) * x.n_kv * x.c_row_tiles;
+    x.c_splits = common_splits(items, (prefix ? prefix->capacity : x.capacity) / COMMON_TILE);
+    if ((items + 8) * x.c_splits > MAX_BLOCKS) return MINF_ERR_SHAPE;
+    const size_t rows = (size_t)items * x.c_splits * 256;
+    p.at_common_ml = p.at_common + up(rows * 128 * sizeof(float));
+    p.at_stat = p.at_common_ml + up(rows * sizeof(float2));
+  }
   p.at_logits = p.need = p.at_stat;
   if (weights != MINF_WEIGHTS_NONE) {
     x.weight = c->weight;
     x.w_sb = c->weight_stride[0]; x.w_sh = c->weight_stride[1];
     x.add_weights = weights == MINF_WEIGHTS_ADD;
     p.at_logits = p.at_stat + up(heads * x.rows * sizeof(float2));
-    p.need = p.at_logits + up(heads * x.max_tiles * x.rows * CACHE_TILE * sizeof(float));
+    p.need = p.at_logits;
+    if (x.rows <= 16) p.need += up(heads * x.max_tiles * x.rows * CACHE_TILE * sizeof(float));
   }
   return MINF_OK;
 }
@@ -175,9 +203,11 @@ minf_status run_plan(const minf_queries *q, const minf_kv_cache *c, const minf_k
   char *w = static_cast<char *>(ws);
   p.x.piece_o = reinterpret_cast<float *>(w);
   p.x.piece_ml = reinterpret_cast<float2 *>(w + p.at_ml);
+  p.x.common_o = reinterpret_cast<float *>(w + p.at_common);
+  p.x.common_ml = reinterpret_cast<float2 *>(w + p.at_common_ml);
   if (weights != MINF_WEIGHTS_NONE) {
     p.x.stat = reinterpret_cast<float2 *>(w + p.at_stat);
-    p.x.logits = reinterpret_cast<float *>(w + p.at_logits);
+    if (p.x.rows <= 16) p.x.logits = reinterpret_cast<float *>(w + p.at_logits);
   }
   return launch_cache_attn(p.x, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? MINF_OK : MINF_ERR_HIP;
 }

@@ -45,16 +45,16 @@ struct CachePart {
 
 template <class X>
 __device__ inline SeqWalk walk_of(X &x, int b) {
-  return seq_walk(x.lens[b], x.capacity, x.n_new, x.n_init, x.n_local);
+  return seq_walk(x.lens[b], x.capacity, x.n_new, x.n_init, x.n_local, x.own_common);
 }
 template <class X>
 __device__ inline SeqWalk walk_of_uniform(X &x, int b) {
-  return seq_walk(uni(x.lens[uni(b)]), x.capacity, x.n_new, x.n_init, x.n_local);
+  return seq_walk(uni(x.lens[uni(b)]), x.capacity, x.n_new, x.n_init, x.n_local, x.own_common);
 }
 // The prefix: every row sees all of it.
 template <class X>
 __device__ inline SeqWalk prefix_walk(X &x) {
-  return seq_walk(x.p_cap > 0 ? uni(x.p_lens[0]) : 0, x.p_cap, 1, 0, x.p_cap);
+  return seq_walk(x.p_cap > 0 ? uni(x.p_lens[0]) : 0, x.p_cap, 1, 0, x.p_cap, x.p_common);
 }
 
 __device__ inline int wave_scan(int v, int lane) {
@@ -239,19 +239,14 @@ __device__ inline bool tile_not_finite(const char *tV, int lane) {
 // (tiles stored one by one: 1M tokens, 8 heads of 4 rows, 963 us; without the stores 717).
 struct CacheLogits {
   char *room;            // CACHE_LOGITS bytes of LDS
-  char *to;              // of the part's next tile in memory; rows of this row tile only
-  int tile_bytes, used, stride;     // rows x 128; bytes waiting; bytes between tiles in memory
+  char *to;              // of the part's next tile in memory
+  int tile_bytes, used;  // rows x 128; bytes waiting
   __device__ inline void flush(int lane) {
-    // (tiles of several row tiles: row by row of tiles)
-    if (stride == tile_bytes) {
-      for (int i = lane * 16; i < used; i += 1024) *reinterpret_cast<uint4 *>(to + i) = *reinterpret_cast<const uint4 *>(room + i);
-    } else {
-      for (int i = lane * 16; i < used; i += 1024) {
-        const int t = i / tile_bytes;
-        *reinterpret_cast<uint4 *>(to + (int64_t)t * stride + (i - t * tile_bytes)) = *reinterpret_cast<const uint4 *>(room + i);
-      }
-    }
-    to += (int64_t)(used / tile_bytes) * stride;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    for (int i = lane * 16; i < used; i += 1024) *reinterpret_cast<uint4 *>(to + i) = *reinterpret_cast<const uint4 *>(room + i);
+    to += used;
     used = 0;
   }
 };
@@ -301,11 +296,11 @@ __device__ inline void update_by_token(CacheRows<NB> &st, const bf16x8 (&p)[NB][
 // across lanes and no rescaling.
 constexpr float REF_ROOM = 16.f;
 
-// One tile of 32 keys from slot kb on.  EDGE: some row may not see some key.  keep: the logits of the part's
-// rows_here rows are wanted.  wait_v awaits the V tile (the K tile is there).
+// One tile of 32 keys from slot kb on.  EDGE: some row may not see some key.  keep: the logits are wanted (one
+// block of rows).  wait_v awaits the V tile (the K tile is there).
 template <int NB, bool EDGE, class WaitV>
 __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, const CacheLane &lo, float c_log2, int kb,
-                                  char *tK, const char *tV, bool keep, CacheLogits &out, int rows_here, int lane, WaitV wait_v) {
+                                  char *tK, const char *tV, bool keep, CacheLogits &out, int lane, WaitV wait_v) {
   f32x4 s[NB][2];
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks)
@@ -382,22 +377,14 @@ __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, cons
           st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][part], st.o[nb][db], 0, 0, 0);
     }
   }
-  if (keep) {
-    const int row = lane & 15;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-      if (16 * nb + row < rows_here) {
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-          *reinterpret_cast<f32x4 *>(out.room + out.used + (16 * nb + row) * 128 + 64 * kt + 16 * (lane >> 4)) = s[nb][kt] * c_log2;
-      }
-    out.used += out.tile_bytes;
-    if (out.used + out.tile_bytes > CACHE_LOGITS) {
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      out.flush(lane);
+  if (NB == 1 && keep) {
+    char *row = out.room + out.used + (lane & 15) * 128 + 16 * (lane >> 4);
+    if (128 * (lane & 15) < out.tile_bytes) {
+      *reinterpret_cast<f32x4 *>(row) = s[0][0] * c_log2;
+      *reinterpret_cast<f32x4 *>(row + 64) = s[0][1] * c_log2;
     }
+    out.used += out.tile_bytes;
+    if (out.used + out.tile_bytes > CACHE_LOGITS) out.flush(lane);
   }
 }
 
@@ -411,7 +398,7 @@ __device__ inline void end_part(X &x, const CachePart &c, const CacheRows<NB> &s
     float l = st.l[nb] + __shfl_xor(st.l[nb], 16);
     l += __shfl_xor(l, 32);
     if (row >= rows) continue;
-    if (whole && x.p_cap == 0) {
+    if (whole && x.direct) {
       const LaneRow a = lane_row(x, c, row);
       const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
       bf16_t *to = x.o + a.b * x.o_sb + (int64_t)(c.kvh * x.group + a.g) * x.o_sh + a.t * x.o_st + 4 * g;
@@ -547,7 +534,6 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
     const int left = g1 - g - (cur.t1 - cur.t0) - SEGMENT_COST;        // tiles of the next one at most
     CachePart nxt;
     CacheMask mask;
-    int rows_here;
     bool keep;
     {
       CacheArgs &x = args_again(args);
@@ -558,12 +544,10 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
       mask.first_pos = cur.prefix ? cur.w.len - 1 : cur.w.i0;
       mask.last_pos = cur.w.len - 1;
       mask.n_tok = cur.prefix ? 1 : x.n_new;
-      rows_here = min(x.rows - cur.rt * NB * 16, NB * 16);
-      keep = x.logits && !cur.prefix;
-      out.tile_bytes = rows_here * CACHE_TILE * 4;
-      out.stride = x.rows * CACHE_TILE * 4;
+      keep = NB == 1 && x.logits && !cur.prefix;
+      out.tile_bytes = x.rows * CACHE_TILE * 4;
       out.to = reinterpret_cast<char *>(x.logits) +
-               ((((int64_t)cur.b * x.n_kv + cur.kvh) * x.max_tiles + cur.t0) * x.rows + cur.rt * NB * 16) * (CACHE_TILE * 4);
+               (((int64_t)cur.b * x.n_kv + cur.kvh) * x.max_tiles + cur.t0) * out.tile_bytes;
     }
     for (int t = cur.t0, kb = cur.w.base(t); t < cur.t1; ++t) {
       const int kb_next = t + 1 == cur.w.T1 ? cur.w.s2 : kb + CACHE_TILE;
@@ -582,20 +566,15 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
         if (more) MINF_WAIT_VMCNT(16); else MINF_WAIT_VMCNT(0);
       };
       char *tK = ring + slot;
-      if (mask.whole(kb)) cache_tile<NB, false>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, rows_here, lane, wait_v);
-      else cache_tile<NB, true>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, rows_here, lane, wait_v);
+      if (mask.whole(kb)) cache_tile<NB, false>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
+      else cache_tile<NB, true>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
       __builtin_amdgcn_s_waitcnt(0xC07F);    // LDS reads done: the slot may be filled again
       slot ^= 2 * HALF_BYTES;
       kb = kb_next;
     }
     {
       CacheArgs &x = args_again(args);
-      if (keep) {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        out.flush(lane);
-      }
+      if (keep) out.flush(lane);
       const bool whole = cur.t0 == 0 && cur.t1 == cur.w.tiles;
       end_part<NB>(x, cur, st, whole, whole ? 2 * x.workers + segment_of(x, cur) : 2 * worker + (g > first_place ? 1 : 0), lane);
     }
@@ -635,17 +614,17 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   const int t = row / x.group, rt = row / tile_rows;
   const bool token = w.i0 + t >= 0;
   const int own0 = uni(pre + before * heads + (kvh * x.row_tiles + rt) * w.places() + SEGMENT_COST);
-  if (x.p_cap == 0 && w.tiles > 0) {
+  if (x.direct && w.tiles > 0) {
     const SegmentPieces p = segment_pieces(own0, own0 + w.tiles, share);
     if (p.first == p.last) return;                                     // written by the worker itself
   }
   float m = -INFINITY, l = 0.f;
   f32x2 o = {0.f, 0.f};
   // pieces from, from + JOIN_WAVES, ... to of a segment
-  auto add = [&](int from, int to, auto place) {
+  auto add = [&](const float2 *all_ml, const float *all_o, int from, int to, auto place) {
     for (int i0 = from; i0 <= to; i0 += 64 * JOIN_WAVES) {
       const int n = min(64, (to - i0) / JOIN_WAVES + 1), i = i0 + JOIN_WAVES * min(lane, n - 1);
-      float2 ml = x.piece_ml[place(i)];
+      float2 ml = all_ml[place(i)];
       if (lane >= n) ml = float2{-INFINITY, 0.f};
       float mx = ml.x;
 #pragma unroll
@@ -664,7 +643,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
         f32x2 po[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          po[j] = *reinterpret_cast<const f32x2 *>(x.piece_o + place(i0 + JOIN_WAVES * min(j0 + j, n - 1)) * D + 2 * lane);
+          po[j] = *reinterpret_cast<const f32x2 *>(all_o + place(i0 + JOIN_WAVES * min(j0 + j, n - 1)) * D + 2 * lane);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float fj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), j0 + j));
@@ -678,15 +657,22 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
     if (tiles <= 0) return;
     const SegmentPieces p = segment_pieces(t0, t0 + tiles, share);
     if (p.first == p.last) {
-      if (wave == 0) add(0, 0, [&](int) { return (int64_t)(2 * x.workers + segment) * x.slot_rows + in_tile; });
+      if (wave == 0) add(x.piece_ml, x.piece_o, 0, 0, [&](int) { return (int64_t)(2 * x.workers + segment) * x.slot_rows + in_tile; });
       return;
     }
-    add(p.first + wave, p.last, [&](int i) { return (int64_t)piece_slot(i, t0, share) * x.slot_rows + in_tile; });
+    add(x.piece_ml, x.piece_o, p.first + wave, p.last, [&](int i) { return (int64_t)piece_slot(i, t0, share) * x.slot_rows + in_tile; });
+  };
+  auto common = [&](const SeqWalk &c, int head, int crow) {
+    const int parts = common_parts(c.s2 / COMMON_TILE, x.c_splits);
+    const int64_t at = ((int64_t)head * x.c_row_tiles + crow / 256) * x.c_splits;
+    add(x.common_ml, x.common_o, wave, parts - 1, [&](int i) { return (at + i) * 256 + crow % 256; });
   };
   if (token) {
+    if (x.own_common) common(w, seg, row);
     join(own0, w.tiles, row - rt * tile_rows, x.n_kv * x.p_row_tiles + (b * x.n_kv + kvh) * x.row_tiles + rt);
     if (x.p_cap > 0) {
       const int prow = b * x.rows + row, prt = prow / tile_rows;
+      if (x.p_common) common(pw, kvh, prow);
       join((kvh * x.p_row_tiles + prt) * pw.places() + SEGMENT_COST, pw.tiles, prow - prt * tile_rows, kvh * x.p_row_tiles + prt);
     }
   }
@@ -739,6 +725,66 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(CacheCall x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (slot + i < w.len) to[i] = x.add_weights ? to[i] + sum[i] : sum[i];
+}
+
+// The same for more than 16 rows, whose logits would be more bytes than the keys: they are computed anew.  A wave
+// takes 64 keys (K as A operands, in registers) and all rows, 16 at a time; per row block 16 MFMAs and 16
+// exponentials a lane.
+constexpr int COLUMN_KEYS = 256;                                // per workgroup
+__global__ __launch_bounds__(256) void cache_column_kernel(CacheCall x) {
+  const int kvh = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
+  const int n = lane & 15, g = lane >> 4, kb = blockIdx.x * COLUMN_KEYS + wave * 64;
+  const int len = uni(min(max(x.lens[b], 0), x.capacity)), i0 = len - x.n_new;
+  if (kb >= len) return;
+  const int64_t head = (int64_t)b * x.n_kv + kvh;
+  bf16x8 k[4][4];                                               // [16 keys][k step]
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt) {
+    const bf16_t *row = x.k + b * x.k_sb + kvh * x.k_sh + (int64_t)min(kb + 16 * kt + n, len - 1) * x.k_st + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) k[kt][ks] = *reinterpret_cast<const bf16x8 *>(row + 32 * ks);
+  }
+  // every row sees every key / no row sees a key
+  const bool whole = kb + 63 <= i0 && (kb + 63 < x.n_init || len - 1 - kb < x.n_local);
+  const bool hidden = kb >= x.n_init && i0 - (kb + 63) >= x.n_local;
+  float sum[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+  for (int r0 = 0; r0 < x.rows && !hidden; r0 += 16) {
+    const int row = min(r0 + n, x.rows - 1), t = row / x.group;
+    const bf16_t *q = x.q + b * x.q_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.q_sh + t * x.q_st + 8 * g;
+    const float2 ml = x.stat[head * x.rows + row];
+    const float inv = r0 + n < x.rows ? ml.y : 0.f, m = ml.x == -INFINITY ? 0.f : ml.x;
+    f32x4 s[4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const bf16x8 qf = *reinterpret_cast<const bf16x8 *>(q + 32 * ks);
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][ks], qf, ks == 0 ? zero : s[kt], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool sees = whole || cache_visible(kb + 16 * kt + 4 * g + i, i0 + t, x.n_init, x.n_local);
+        const float p = fast_exp2(fmaf(s[kt][i], x.c_log2, -m)) * inv;
+        sum[4 * kt + i] += sees && inv != 0.f ? p : 0.f;
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) sum[i] += __shfl_xor(sum[i], d);
+  if (n != 0) return;
+  float *to = x.weight + b * x.w_sb + kvh * x.w_sh;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int key = kb + 16 * (i >> 2) + 4 * g + (i & 3);
+    if (key < len) to[key] = x.add_weights ? to[key] + sum[i] : sum[i];
+  }
 }
 
 // ---- eviction ---------------------------------------------------------------------------------------------
@@ -1036,10 +1082,16 @@ static hipError_t launch_workers(const CacheCall &x, hipStream_t st) {
 }
 
 hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
-  hipError_t e = x.row_blocks == 1 ? launch_workers<1>(x, st) : launch_workers<2>(x, st);
+  hipError_t e = x.p_common || x.own_common ? launch_cache_common(x, st) : hipSuccess;
+  if (e != hipSuccess) return e;
+  e = x.row_blocks == 1 ? launch_workers<1>(x, st) : launch_workers<2>(x, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(cache_join_kernel, dim3(x.batch * x.n_kv * x.rows), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks);
   if ((e = hipGetLastError()) != hipSuccess || !x.weight) return e;
+  if (!x.logits) {
+    hipLaunchKernelGGL(cache_column_kernel, dim3((x.capacity + COLUMN_KEYS - 1) / COLUMN_KEYS, x.n_kv, x.batch), dim3(256), 0, st, x);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(cache_weight_kernel, dim3((x.capacity + 1023) / 1024, x.n_kv, x.batch), dim3(256), 0, st, x);
   return hipGetLastError();
 }

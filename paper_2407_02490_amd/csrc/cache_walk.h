@@ -17,7 +17,7 @@
 
 namespace minf {
 
-constexpr int CACHE_TILE = 32;
+constexpr int CACHE_TILE = 32, COMMON_TILE = 64;
 // A segment (below) costs a worker its tiles and, for its rows and its result, as much as two more: it takes up so
 // many places more in the list, in front of its tiles.
 constexpr int SEGMENT_COST = 2;
@@ -36,11 +36,20 @@ struct SeqWalk {
   }
 };
 
-// n_init, n_local: at most the capacity, so that no sum here leaves 32 bits.
-MINF_HD SeqWalk seq_walk(int32_t len, int32_t capacity, int32_t n_new, int32_t n_init, int32_t n_local) {
+// n_init, n_local: at most the capacity, so that no sum here leaves 32 bits.  behind_common: only what lies behind
+// the slots that every row sees, in whole tiles of 64 (n_local: the capacity); those are another kernel's.
+MINF_HD int32_t common_slots(int32_t i0) { return i0 < 0 ? 0 : (i0 + 1) / COMMON_TILE * COMMON_TILE; }
+MINF_HD SeqWalk seq_walk(int32_t len, int32_t capacity, int32_t n_new, int32_t n_init, int32_t n_local,
+                         bool behind_common = false) {
   SeqWalk w;
   w.len = len < 0 ? 0 : (len > capacity ? capacity : len);
   w.i0 = w.len - n_new;
+  if (behind_common) {
+    w.e1 = w.T1 = 0;
+    w.lo = w.s2 = common_slots(w.i0);
+    w.tiles = (w.len - w.s2 + CACHE_TILE - 1) / CACHE_TILE;
+    return w;
+  }
   w.e1 = n_init < w.len ? n_init : w.len;
   w.lo = w.i0 - n_local + 1;
   if (w.lo < 0) w.lo = 0;
@@ -75,6 +84,13 @@ MINF_HD SegmentPieces segment_pieces(int32_t t0, int32_t t1, int32_t share) {
 }
 MINF_HD int32_t piece_slot(int32_t worker, int32_t t0, int32_t share) {
   return 2 * worker + (t0 > worker * share ? 1 : 0);
+}
+
+// The common slots of a segment are cut into at most `splits` parts of equally many tiles: tiles per part.
+MINF_HD int32_t common_share(int32_t tiles, int32_t splits) { return (tiles + splits - 1) / splits; }
+MINF_HD int32_t common_parts(int32_t tiles, int32_t splits) {
+  const int32_t per = common_share(tiles, splits);
+  return per > 0 ? (tiles + per - 1) / per : 0;
 }
 
 }  // namespace minf

@@ -47,11 +47,16 @@ def attention(q, k, v, n, n_init, n_local, scale=None, pk=None, pv=None):
     return o, w, mag, slack
 
 
-def check_o(got, want, mag, slack, what=""):
-    """bf16 output: half a step of the value (2^-8), P as two bf16 (2^-16 of each term), the p's own error."""
+P_TWO_BF16 = 2.0 ** -16    # P as the sum of two bf16: what is left of p after one half step is rounded again
+P_BF16 = 2.0 ** -8         # P as one bf16 (slots that more than 32 rows see): off by half a step, 2^-8 of the value
+
+
+def check_o(got, want, mag, slack, what="", p_step=P_TWO_BF16):
+    """bf16 output: half a step of the value (2^-8); every p_ij that multiplies v_j is off by p_step of itself, which
+    moves the output by at most p_step * sum_j p_ij |v_j|; the p's own error in the same way."""
     got = f64(got)
     assert np.isfinite(got).all(), f"{what}: not finite"
-    bound = 2.0 ** -8 * np.abs(want) + (1 + 2.0 ** -8) * (2.0 ** -16 + slack[..., None]) * mag + 1e-30
+    bound = 2.0 ** -8 * np.abs(want) + (1 + 2.0 ** -8) * (p_step + slack[..., None]) * mag + 1e-30
     over = np.abs(got - want) / bound
     assert over.max(initial=0.0) <= 1.0, f"{what}: error {over.max():.3g} times its bound at {np.unravel_index(over.argmax(), over.shape)}"
 

@@ -55,6 +55,27 @@ static int walks() {
   return cases;
 }
 
+// Behind the common slots: the tiles and they together hold every slot once, and every row sees all common ones.
+static int common() {
+  int cases = 0;
+  for (int cap : {1, 64, 65, 200, 1000})
+    for (int T : {1, 2, 40, 64})
+      for (int len = 0; len <= cap; len += (cap > 100 ? 13 : 1)) {
+        ++cases;
+        const SeqWalk w = seq_walk(len, cap, T, 0, cap, true);
+        const int c = common_slots(w.i0);
+        CHECK(c % 64 == 0 && c >= 0 && c <= len && w.base(0) == c);
+        CHECK(c == 0 || c - 1 <= w.i0);
+        CHECK(c + w.tiles * CACHE_TILE >= len && c + (w.tiles - 1) * CACHE_TILE < len + (len == 0));
+        CHECK((w.len - c) <= T + 63);
+        for (int splits : {1, 2, 7, 64}) {
+          const int tiles = c / 64, per = common_share(tiles, splits), parts = common_parts(tiles, splits);
+          CHECK(parts <= splits && parts * per >= tiles && (tiles == 0 ? parts == 0 : (parts - 1) * per < tiles));
+        }
+      }
+  return cases;
+}
+
 static int shares() {
   int cases = 0;
   const std::vector<std::vector<int>> lists = {{1}, {5, 0, 3}, {40, 1, 1, 1, 300, 2}, {0, 0}, {7, 7, 7, 7, 7, 7, 7}, {5000}};
@@ -91,7 +112,7 @@ static int shares() {
 }
 
 int main() {
-  const int a = walks(), b = shares();
-  if (fails == 0) printf("ok walks %d shares %d\n", a, b);
+  const int a = walks(), b = shares(), c = common();
+  if (fails == 0) printf("ok walks %d shares %d common %d\n", a, b, c);
   return fails != 0;
 }
