@@ -6,6 +6,7 @@ the shared library has not been built, importing the entry points raises.
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -334,42 +335,41 @@ class KVCache:
     """Keys and values of a batch of sequences, with their lengths (see minf_kv_cache): k, v
     [B, Hkv, capacity, 128] bf16 in any strides with head_dim contiguous, or [Hkv, capacity, 128]
     (one sequence); lens [B] int32; weight [B, Hkv, capacity] float32 (without B as k) or None.
-    Keeps the tensors; copies nothing.  K and V of a prefill are such a cache as they are."""
+    Keeps the tensors, which must keep their storage; copies nothing.  K and V of a prefill are such a
+    cache as they are."""
 
     def __init__(self, k, v, lens, weight=None):
-        self.k, self.v, self.lens, self.weight = k, v, lens, weight
-
-    def _args(self):
-        batch = self.k.shape[0] if self.k.dim() == 4 else 1
-        return batch, self.k.shape[-3], self.k.shape[-2]
-
-    @property
-    def batch(self):
-        return self._args()[0]
-
-    @property
-    def capacity(self):
-        return self._args()[2]
-
-    def c_struct(self):
-        batch, heads, cap = self._args()
-        k, v, lens, w = self.k, self.v, self.lens, self.weight
         assert k.dim() in (3, 4) and k.shape == v.shape, "k and v: [B, Hkv, capacity, 128] or [Hkv, capacity, 128]"
         for t in (k, v):
             assert t.dtype == torch.bfloat16 and t.stride(-1) == 1, "bf16, head_dim contiguous"
+        batch = k.shape[0] if k.dim() == 4 else 1
         assert lens.dtype == torch.int32 and lens.shape == (batch,) and lens.is_contiguous(), "lens: int32 [B]"
-        for t in (v, lens) + (() if w is None else (w,)):
+        for t in (v, lens) + (() if weight is None else (weight,)):
             assert t.device == k.device, "one device"
         s = _KVCache()
         s.k, s.v, s.lens = k.data_ptr(), v.data_ptr(), lens.data_ptr()
         s.k_stride[:], s.v_stride[:] = _strides4(k)[0], _strides4(v)[0]
-        if w is not None:
-            assert w.dtype == torch.float32 and w.shape == k.shape[:-1] and w.stride(-1) == 1, \
+        if weight is not None:
+            assert weight.dtype == torch.float32 and weight.shape == k.shape[:-1] and weight.stride(-1) == 1, \
                 "weight: float32 [B, Hkv, capacity], slots contiguous"
-            s.weight = w.data_ptr()
-            s.weight_stride[:] = (0, w.stride(0)) if w.dim() == 2 else (w.stride(0), w.stride(1))
-        s.batch, s.n_kv_heads, s.capacity, s.head_dim = batch, heads, cap, k.shape[-1]
-        return s
+            s.weight = weight.data_ptr()
+            s.weight_stride[:] = (0, weight.stride(0)) if weight.dim() == 2 else (weight.stride(0), weight.stride(1))
+        s.batch, s.n_kv_heads, s.capacity, s.head_dim = batch, k.shape[-3], k.shape[-2], k.shape[-1]
+        self._tensors, self._struct, self._ref = (k, v, lens, weight), s, ctypes.byref(s)
+
+    def _tensor(i):
+        def replace(self, t):                    # cache.lens += 1 comes here with the tensor itself
+            assert t is self._tensors[i], "a cache keeps its tensors: make another KVCache"
+        return property(lambda self: self._tensors[i], replace)
+
+    k, v, lens, weight = _tensor(0), _tensor(1), _tensor(2), _tensor(3)
+    device = property(lambda self: self._tensors[0].device)
+    batch = property(lambda self: self._struct.batch)
+    n_kv_heads = property(lambda self: self._struct.n_kv_heads)
+    capacity = property(lambda self: self._struct.capacity)
+
+    def c_struct(self):
+        return self._struct
 
 
 def alloc_kv_cache(batch, n_kv_heads, capacity, weight=True, device="cuda"):
@@ -383,68 +383,75 @@ def alloc_kv_cache(batch, n_kv_heads, capacity, weight=True, device="cuda"):
 _WEIGHTS = {None: 0, "set": 1, "add": 2}
 
 
+_QUERIES = struct.Struct("PPqqqqqqiif4x")               # minf_queries
+
+
 def _queries(q, o, cache, scale):
     """q, o: [B, Hq, n_new, 128] ([Hq, n_new, 128] with a cache of one sequence)."""
-    x = _Queries()
-    for t in (q, o):
-        if t is not None:
-            assert t.dtype == torch.bfloat16 and t.stride(-1) == 1, "bf16, head_dim contiguous"
-            assert t.dim() in (3, 4) and t.shape == q.shape and t.device == cache.k.device, "o like q, on the cache's device"
-    assert (q.shape[0] if q.dim() == 4 else 1) == cache.batch and q.shape[-1] == cache.k.shape[-1], "q and cache differ"
-    x.q, x.o = q.data_ptr(), o.data_ptr() if o is not None else None
-    x.q_stride[:] = _strides4(q)[0]
-    x.o_stride[:] = _strides4(o)[0] if o is not None else (0, 0, 0)
-    x.n_q_heads, x.n_new, x.softmax_scale = q.shape[-3], q.shape[-2], float(scale)
-    return x
+    assert q.dtype == torch.bfloat16, "bf16"
+    shape, st = q.shape, q.stride()
+    if len(shape) == 3:
+        shape, st = (1, *shape), (0, *st)
+    batch, heads, n_new, d = shape
+    assert batch == cache._struct.batch and d == cache._struct.head_dim and q.device == cache.device, "q and cache differ"
+    ot, to = st, 0
+    if o is not None:
+        assert o.dtype == torch.bfloat16 and o.shape == q.shape and o.device == q.device, "o like q"
+        ot, to = o.stride() if o.dim() == 4 else (0, *o.stride()), o.data_ptr()
+    assert st[3] == 1 and ot[3] == 1, "head_dim contiguous"
+    return _Queries.from_buffer_copy(_QUERIES.pack(q.data_ptr(), to, st[0], st[1], st[2], ot[0], ot[1], ot[2], heads, n_new, scale))
 
 
-def _cache_call(fn, device, ws, stream, *args):
-    """On the tensors' device, its current stream unless another one is given."""
-    assert ws.device == device, "workspace on the cache's device"
-    with torch.cuda.device(device):
-        _check(fn(*args, ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size(), _stream(stream)))
+def _cache_call(fn, cache, ws, stream, *args):
+    """On the cache's device, its current stream unless another one is given."""
+    dev = cache.device
+    assert ws.device == dev and ws.is_contiguous(), "workspace: contiguous, on the cache's device"
+    raw = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == dev.index:
+        status = fn(*args, ws.data_ptr(), ws.numel() * ws.element_size(), raw)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, ws.data_ptr(), ws.numel() * ws.element_size(), raw)
+    _check(status)
+
+
+def _weights(weights):
+    assert weights in _WEIGHTS, 'weights: None, "set" or "add"'
+    return _WEIGHTS[weights]
 
 
 def minf_cache_attn_workspace_bytes(q, cache, n_init=0, n_local=None, weights=None):
-    x, c = _queries(q, None, cache, 0.0), cache.c_struct()
-    return int(lib().minf_cache_attn_workspace_bytes(ctypes.byref(x), ctypes.byref(c), n_init,
-                                                     cache.capacity if n_local is None else n_local, _WEIGHTS[weights]))
+    return int(lib().minf_cache_attn_workspace_bytes(ctypes.byref(_queries(q, None, cache, 0.0)), cache._ref, n_init,
+                                                     cache.capacity if n_local is None else n_local, _weights(weights)))
 
 
 def minf_prefix_attn_workspace_bytes(q, prefix, cache):
-    x, p, c = _queries(q, None, cache, 0.0), prefix.c_struct(), cache.c_struct()
-    return int(lib().minf_prefix_attn_workspace_bytes(ctypes.byref(x), ctypes.byref(p), ctypes.byref(c)))
+    return int(lib().minf_prefix_attn_workspace_bytes(ctypes.byref(_queries(q, None, cache, 0.0)), prefix._ref, cache._ref))
 
 
 def minf_cache_evict_workspace_bytes(cache, keep):
-    c = cache.c_struct()
-    return int(lib().minf_cache_evict_workspace_bytes(ctypes.byref(c), keep))
+    return int(lib().minf_cache_evict_workspace_bytes(cache._ref, keep))
 
 
 def minf_cache_attn(q, o, cache, ws, n_init=0, n_local=None, weights=None, scale=0.0, stream=None):
     """o = attention of the newest tokens q against the cache, sink + sliding window (n_local=None: the
     whole cache); weights="set" / "add": cache.weight receives the attention weight of every slot."""
-    x, c = _queries(q, o, cache, scale), cache.c_struct()
-    _cache_call(lib().minf_cache_attn, cache.k.device, ws, stream, ctypes.byref(x), ctypes.byref(c), n_init,
-                cache.capacity if n_local is None else n_local, _WEIGHTS[weights])
+    _cache_call(lib().minf_cache_attn, cache, ws, stream, ctypes.byref(_queries(q, o, cache, scale)), cache._ref, n_init,
+                cache.capacity if n_local is None else n_local, _weights(weights))
 
 
 def minf_prefix_attn(q, o, prefix, cache, ws, scale=0.0, stream=None):
     """o = attention of the newest tokens q against a prefix that all sequences share (a cache of one
     sequence) and, behind it, their own caches."""
-    assert prefix.k.device == cache.k.device, "one device"
-    x, p, c = _queries(q, o, cache, scale), prefix.c_struct(), cache.c_struct()
-    _cache_call(lib().minf_prefix_attn, cache.k.device, ws, stream, ctypes.byref(x), ctypes.byref(p), ctypes.byref(c))
+    assert prefix.device == cache.device, "one device"
+    _cache_call(lib().minf_prefix_attn, cache, ws, stream, ctypes.byref(_queries(q, o, cache, scale)), prefix._ref, cache._ref)
 
 
 def minf_cache_evict(cache, keep, ws, kept, to=None, n_init=0, n_recent=0, stream=None):
     """Keeps, per sequence and K/V head, `keep` slots: the first n_init, the last n_recent and those of the
     largest weight; moves them to the front of `to` (None: in place).  kept [B, Hkv, keep] int32."""
     to = cache if to is None else to
-    batch, heads, _ = cache._args()
-    assert kept.dtype == torch.int32 and kept.is_contiguous() and kept.numel() == batch * heads * keep, \
+    assert kept.dtype == torch.int32 and kept.is_contiguous() and kept.numel() == cache.batch * cache.n_kv_heads * keep, \
         "kept: int32 [B, Hkv, keep]"
-    assert kept.device == cache.k.device and to.k.device == cache.k.device, "one device"
-    c, t = cache.c_struct(), to.c_struct()
-    _cache_call(lib().minf_cache_evict, cache.k.device, ws, stream, ctypes.byref(c), n_init, n_recent, keep,
-                ctypes.byref(t), ctypes.c_void_p(kept.data_ptr()))
+    assert kept.device == cache.device and to.device == cache.device, "one device"
+    _cache_call(lib().minf_cache_evict, cache, ws, stream, cache._ref, n_init, n_recent, keep, to._ref, kept.data_ptr())

@@ -144,7 +144,7 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
     segments += (int64_t)x.n_kv * x.p_row_tiles;
     places += (int64_t)x.n_kv * x.p_row_tiles * ((prefix->capacity + CACHE_TILE - 1) / CACHE_TILE + SEGMENT_COST);
   }
-  if (places >= (int64_t)1 << 31) return MINF_ERR_SHAPE;               // the list of tiles is counted in 32 bits
+  if (places >= (int64_t)1 << 30) return MINF_ERR_SHAPE;               // the list of tiles is counted in 32 bits
   x.workers = CUS * 4;
   // workspace: O of the pieces, their maxima and sums, the same of the common slots' parts, statistics of the
   // rows, logits (for the weights of up to 16 rows)
@@ -165,6 +165,7 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   }
   p.at_logits = p.need = p.at_stat;
   if (weights != MINF_WEIGHTS_NONE) {
+    if ((int64_t)heads * (x.rows + (x.capacity + 1023) / 1024) > MAX_BLOCKS) return MINF_ERR_SHAPE;
     x.weight = c->weight;
     x.w_sb = c->weight_stride[0]; x.w_sh = c->weight_stride[1];
     x.add_weights = weights == MINF_WEIGHTS_ADD;

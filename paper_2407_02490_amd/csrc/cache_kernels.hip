@@ -18,7 +18,7 @@
 
 namespace minf {
 
-constexpr int CACHE_WAVES = 4;                                  // per workgroup
+constexpr int CACHE_WAVES = WORKER_GROUP;                       // per workgroup
 constexpr int CACHE_RING = 2 * 2 * HALF_BYTES;                  // per wave: two slots of a K and a V tile
 constexpr int CACHE_LOGITS = 8192;                              // per wave: logits on their way out
 static_assert(CACHE_TILE * ROW_BYTES == HALF_BYTES, "a tile of the walk is half a 64-key tile");
@@ -43,13 +43,20 @@ struct CachePart {
   SeqWalk w;             // of the sequence (or of the prefix)
 };
 
+// Lengths: `mine` holds those of the first 64 sequences, one a lane, loaded once.
 template <class X>
-__device__ inline SeqWalk walk_of(X &x, int b) {
-  return seq_walk(x.lens[b], x.capacity, x.n_new, x.n_init, x.n_local, x.own_common);
+__device__ inline SeqWalk walk_of_len(X &x, int len) {
+  return seq_walk(len, x.capacity, x.n_new, x.n_init, x.n_local, x.own_common);
 }
 template <class X>
-__device__ inline SeqWalk walk_of_uniform(X &x, int b) {
-  return seq_walk(uni(x.lens[uni(b)]), x.capacity, x.n_new, x.n_init, x.n_local, x.own_common);
+__device__ inline int first_lens(X &x, int lane) { return lane < x.batch ? x.lens[lane] : 0; }
+template <class X>
+__device__ inline int places_of(X &x, int b, int mine) {       // b: 64 i + lane
+  return b < x.batch ? walk_of_len(x, b < 64 ? mine : x.lens[b]).places() : 0;
+}
+template <class X>
+__device__ inline SeqWalk walk_of(X &x, int b, int mine) {     // wave-uniform
+  return walk_of_len(x, b < 64 ? __builtin_amdgcn_readlane(mine, b) : uni(x.lens[uni(b)]));
 }
 // The prefix: every row sees all of it.
 template <class X>
@@ -66,19 +73,27 @@ __device__ inline int wave_scan(int v, int lane) {
   return v;
 }
 
-// Places of all sequences in the list, per K/V head and row tile.
+// Places of all sequences in the list, and of those in front of sequence b, per K/V head and row tile.
 template <class X>
-__device__ inline int all_places(X &x, int lane) {
-  int sum = 0;
-  for (int b0 = 0; b0 < x.batch; b0 += 64) sum += b0 + lane < x.batch ? walk_of(x, b0 + lane).places() : 0;
+__device__ inline void count_places(X &x, int b, int mine, int lane, int &all, int &before) {
+  all = before = 0;
+  for (int b0 = 0; b0 < x.batch; b0 += 64) {
+    const int t = places_of(x, b0 + lane, mine);
+    all += t;
+    before += b0 + lane < b ? t : 0;
+  }
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-  return uni(sum);
+  for (int d = 32; d > 0; d >>= 1) {
+    all += __shfl_xor(all, d);
+    before += __shfl_xor(before, d);
+  }
+  all = uni(all);
+  before = uni(before);
 }
 
 // The part that begins at place g of the list, of those before place g1 (none: t0 >= t1); pre: places of the prefix.
 template <class X>
-__device__ inline CachePart seek(X &x, int &g, int g1, int pre, int lane) {
+__device__ inline CachePart seek(X &x, int &g, int g1, int pre, int mine, int lane) {
   CachePart c;
   int s, at = g;
   if (g < pre) {
@@ -94,7 +109,7 @@ __device__ inline CachePart seek(X &x, int &g, int g1, int pre, int lane) {
     c.prefix = 0;
     c.b = 0;
     for (int b0 = 0; b0 < x.batch; b0 += 64) {
-      const int i = b0 + lane, t = i < x.batch ? walk_of(x, i).places() : 0;
+      const int t = places_of(x, b0 + lane, mine);
       const int incl = wave_scan(t, lane);
       const unsigned long long beyond = __builtin_amdgcn_ballot_w64((before + incl) * heads > at);
       if (beyond != 0) {
@@ -105,7 +120,7 @@ __device__ inline CachePart seek(X &x, int &g, int g1, int pre, int lane) {
       }
       before += uni(__shfl(incl, 63));
     }
-    c.w = walk_of_uniform(x, c.b);
+    c.w = walk_of(x, c.b, mine);
     at -= before * heads;
     s = uni(at / c.w.places());
     at -= s * c.w.places();
@@ -121,14 +136,14 @@ __device__ inline CachePart seek(X &x, int &g, int g1, int pre, int lane) {
 
 // The part behind c, of at most `most` tiles.
 template <class X>
-__device__ inline CachePart next_part(X &x, CachePart c, int most) {
+__device__ inline CachePart next_part(X &x, CachePart c, int most, int mine) {
   c.t0 = 0;
   if (++c.rt >= (c.prefix ? x.p_row_tiles : x.row_tiles)) {
     c.rt = 0;
     if (++c.kvh >= x.n_kv) {
       c.kvh = 0;
       if (c.prefix) { c.prefix = 0; c.b = -1; }
-      do c.w = walk_of_uniform(x, ++c.b);
+      do c.w = walk_of(x, ++c.b, mine);
       while (c.w.tiles == 0);                  // there is one: the list goes on
     }
   }
@@ -411,7 +426,7 @@ __device__ inline void end_part(X &x, const CachePart &c, const CacheRows<NB> &s
         two.y = __builtin_bit_cast(unsigned, __builtin_convertvector(w, bf16x2));
         *reinterpret_cast<uint2 *>(to + 16 * db) = two;
       }
-      if (x.stat && g == 0) x.stat[((int64_t)c.b * x.n_kv + c.kvh) * x.rows + row] = float2{st.m[nb], inv};
+      if (x.stat && g == 0) x.stat[((int64_t)c.b * x.n_kv + c.kvh) * x.rows + row] = float2{st.m[nb], l};
       continue;
     }
     const int64_t at = (int64_t)slot * x.slot_rows + nb * 16 + n;
@@ -419,6 +434,48 @@ __device__ inline void end_part(X &x, const CachePart &c, const CacheRows<NB> &s
     float *to = x.piece_o + at * D + 4 * g;
 #pragma unroll
     for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(to + 16 * db) = st.o[nb][db];
+  }
+}
+
+// The same for the four waves of a workgroup whose parts are one segment's: their pieces become one.  lds: the rings.
+template <int NB, class X>
+__device__ inline void end_group(X &x, const CachePart &c, const CacheRows<NB> &st, char *lds, int lane) {
+  constexpr int ROW = D * 4 + 16;                                      // 16 bytes between rows: banks
+  constexpr int AT_ML = 16 * NB * ROW;
+  const int n = lane & 15, g = lane >> 4, wave = uni(threadIdx.x >> 6);
+  char *room = lds + wave * CACHE_RING;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    float l = st.l[nb] + __shfl_xor(st.l[nb], 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) *reinterpret_cast<float2 *>(room + AT_ML + (16 * nb + n) * 8) = float2{st.m[nb], l};
+#pragma unroll
+    for (int db = 0; db < 8; ++db)
+      *reinterpret_cast<f32x4 *>(room + (16 * nb + n) * ROW + (16 * db + 4 * g) * 4) = st.o[nb][db];
+  }
+  __syncthreads();
+  const int first = c.rt * NB * 16, rows = min((c.prefix ? x.batch * x.rows : x.rows) - first, 16 * NB);
+  const int64_t slot = 2 * WORKER_GROUP * (int64_t)blockIdx.x;
+  for (int i = threadIdx.x; i < rows * 32; i += 64 * CACHE_WAVES) {
+    const int row = i >> 5, d = 4 * (i & 31);
+    float2 ml[CACHE_WAVES];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < CACHE_WAVES; ++w) {
+      ml[w] = *reinterpret_cast<const float2 *>(lds + w * CACHE_RING + AT_ML + row * 8);
+      m = fmaxf(m, ml[w].x);
+    }
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < CACHE_WAVES; ++w) {
+      if (ml[w].x == -INFINITY && ml[w].y == 0.f) continue;            // no visible key
+      const float f = fast_exp2(ml[w].x - m);
+      l += ml[w].y * f;
+      o += *reinterpret_cast<const f32x4 *>(lds + w * CACHE_RING + row * ROW + d * 4) * f;
+    }
+    const int64_t at = slot * x.slot_rows + row;
+    if (d == 0) x.piece_ml[at] = float2{m, l};
+    *reinterpret_cast<f32x4 *>(x.piece_o + at * D + d) = o;
   }
 }
 
@@ -494,17 +551,20 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
   char *ring = lds + wave * CACHE_RING;
   const unsigned ring_at = uni(lds_addr_of(ring));
 
-  int first_place, g, g1;                    // place of the current part's first tile, end of this worker's places
+  int first_place, g, g1, share;             // place of the current part's first tile, end of this worker's places
+  const int mine = first_lens(*args, lane);
   CachePart cur;
   {
     CacheArgs &x = args_again(args);
     const int pre = prefix_walk(x).places() * x.n_kv * x.p_row_tiles;
-    const int total = pre + all_places(x, lane) * x.n_kv * x.row_tiles;
-    const int share = worker_share(total, x.workers);
+    int all, before;
+    count_places(x, 0, mine, lane, all, before);
+    const int total = pre + all * x.n_kv * x.row_tiles;
+    share = worker_share(total, x.workers);
     first_place = g = worker * share;
     g1 = min(g + share, total);
     if (g >= g1) return;
-    cur = seek(x, g, g1, pre, lane);
+    cur = seek(x, g, g1, pre, mine, lane);
     if (cur.t0 >= cur.t1) return;
   }
   CacheSource src;
@@ -537,7 +597,7 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
     bool keep;
     {
       CacheArgs &x = args_again(args);
-      if (left > 0) nxt = next_part(x, cur, left);
+      if (left > 0) nxt = next_part(x, cur, left, mine);
       begin_part<NB>(x, cur, st, lane);
       mask.n_init = cur.prefix ? 0 : x.n_init;
       mask.n_local = cur.prefix ? x.p_cap : x.n_local;
@@ -575,6 +635,11 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
     {
       CacheArgs &x = args_again(args);
       if (keep) out.flush(lane);
+      const int t0 = g - cur.t0;
+      if (group_inside(blockIdx.x, t0, t0 + cur.w.tiles, share)) {     // the four waves' only part
+        end_group<NB>(x, cur, st, lds, lane);
+        break;
+      }
       const bool whole = cur.t0 == 0 && cur.t1 == cur.w.tiles;
       end_part<NB>(x, cur, st, whole, whole ? 2 * x.workers + segment_of(x, cur) : 2 * worker + (g > first_place ? 1 : 0), lane);
     }
@@ -587,93 +652,154 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
 
 // ---- joining the pieces ---------------------------------------------------------------------------------
 // One workgroup per output row: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the pieces of the row's
-// own segment and of the prefix's.  A wave takes every fourth piece: first the references and sums of up to 64
-// of them at once (a lane each), then their O rows (two d a lane).  Rows without a visible key, or without a
-// token, give zeros.
-constexpr int JOIN_WAVES = 4;
-__global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x, int tile_rows) {
+// own segment, of the prefix's and of the common slots.  A wave takes every fourth piece, eight at a time with all
+// their loads in flight.  Rows without a visible key, or without a token, give zeros.
+// Further workgroups give the slots their weights (where the logits were kept): they need the references and sums
+// of a K/V head's rows, which they join themselves, rather than wait for another launch.
+constexpr int JOIN_WAVES = 4, JOIN_AHEAD = 8;
+
+// The pieces that the workers left of a segment.
+struct PieceList {
+  SegmentPieces p;
+  int t0, share, segment;
+  int64_t base;                            // row of slot 0
+  int slot_rows, workers;
+  __device__ inline int count() const { return p.first == p.last ? 1 : p.count(); }
+  __device__ inline int64_t at(int i) const {
+    const int slot = p.first == p.last ? 2 * workers + segment : piece_slot(p.worker(i), t0, share);
+    return (int64_t)slot * slot_rows + base;
+  }
+};
+
+__global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x, int tile_rows, int joins) {
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
-  const int row = blockIdx.x % x.rows, seg = blockIdx.x / x.rows;      // of the sequence and K/V head
+  const bool joining = (int)blockIdx.x < joins;
+  // joining: the row of a K/V head of a sequence; else 1024 slots of one
+  const int per_head = joining ? x.rows : (x.capacity + 1023) / 1024, id = joining ? blockIdx.x : blockIdx.x - joins;
+  const int seg = id / per_head, item = id - seg * per_head;
   const int b = seg / x.n_kv, kvh = seg - b * x.n_kv;
+  const int mine = first_lens(x, lane);
   const SeqWalk pw = prefix_walk(x);
   const int pre = pw.places() * x.n_kv * x.p_row_tiles;
   const int heads = x.n_kv * x.row_tiles;
-  int before = 0, all = 0;
-  for (int b0 = 0; b0 < x.batch; b0 += 64) {
-    const int i = b0 + lane, t = i < x.batch ? walk_of(x, i).places() : 0;
-    all += t;
-    before += i < b ? t : 0;
-  }
+  int all, before;
+  count_places(x, b, mine, lane, all, before);
+  const int share = worker_share(pre + all * heads, x.workers);
+  const SeqWalk w = walk_of(x, b, mine);
+  auto own_pieces = [&](int row) {
+    const int rt = row / tile_rows;
+    PieceList l;
+    l.t0 = pre + before * heads + (kvh * x.row_tiles + rt) * w.places() + SEGMENT_COST;
+    l.p = segment_pieces(l.t0, l.t0 + w.tiles, share);
+    l.share = share; l.segment = x.n_kv * x.p_row_tiles + seg * x.row_tiles + rt;
+    l.base = row - rt * tile_rows; l.slot_rows = x.slot_rows; l.workers = x.workers;
+    return l;
+  };
+
+  if (!joining) {
+    // weights of 1024 slots, four of a tile a thread (slots and tiles are aligned alike); up to 16 rows
+    if (item * 1024 >= w.len) return;
+    __shared__ float2 stat[16];
+    const PieceList l = own_pieces(0);
+    const bool whole = w.tiles > 0 && l.p.first == l.p.last;
+    for (int row = wave; row < x.rows; row += JOIN_WAVES) {
+      float m = -INFINITY, sum = 0.f;
+      const int n = l.count();
+      for (int i0 = 0; i0 < n; i0 += 64) {
+        float2 ml = float2{-INFINITY, 0.f};
+        if (i0 + lane < n) ml = whole ? x.stat[(int64_t)seg * x.rows + row] : x.piece_ml[l.at(i0 + lane) + row];
+        float mx = ml.x;
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    all += __shfl_xor(all, d);
-    before += __shfl_xor(before, d);
+        for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+        mx = fmaxf(mx, m);
+        sum = m == -INFINITY && sum == 0.f ? 0.f : sum * fast_exp2(m - mx);
+        float f = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.y * fast_exp2(ml.x - mx);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) f += __shfl_xor(f, d);
+        sum += f;
+        m = mx;
+      }
+      if (lane == 0) stat[row] = float2{m, sum > 0.f || sum != sum ? 1.0f / sum : 0.f};
+    }
+    __syncthreads();
+    const int slot = item * 1024 + 4 * threadIdx.x;
+    if (slot >= w.len) return;
+    const int tau = w.tile_of(slot);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (tau >= 0) {
+      const float *s = x.logits + ((int64_t)seg * x.max_tiles + tau) * (x.rows * CACHE_TILE) + (slot - w.base(tau));
+#pragma unroll 4
+      for (int r = 0; r < x.rows; ++r) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(s + r * CACHE_TILE);
+        const float2 ml = stat[r];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += v[i] == -INFINITY ? 0.f : fast_exp2(v[i] - ml.x) * ml.y;
+      }
+    }
+    float *to = x.weight + b * x.w_sb + kvh * x.w_sh + slot;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (slot + i < w.len) to[i] = x.add_weights ? to[i] + sum[i] : sum[i];
+    return;
   }
-  const int share = worker_share(uni(pre + all * heads), x.workers);
-  const SeqWalk w = walk_of_uniform(x, b);
-  const int t = row / x.group, rt = row / tile_rows;
+
+  const int row = item, t = row / x.group;
   const bool token = w.i0 + t >= 0;
-  const int own0 = uni(pre + before * heads + (kvh * x.row_tiles + rt) * w.places() + SEGMENT_COST);
-  if (x.direct && w.tiles > 0) {
-    const SegmentPieces p = segment_pieces(own0, own0 + w.tiles, share);
-    if (p.first == p.last) return;                                     // written by the worker itself
-  }
+  const PieceList own = own_pieces(row);
+  if (x.direct && w.tiles > 0 && own.p.first == own.p.last) return;    // written by the worker itself
   float m = -INFINITY, l = 0.f;
   f32x2 o = {0.f, 0.f};
-  // pieces from, from + JOIN_WAVES, ... to of a segment
-  auto add = [&](const float2 *all_ml, const float *all_o, int from, int to, auto place) {
-    for (int i0 = from; i0 <= to; i0 += 64 * JOIN_WAVES) {
-      const int n = min(64, (to - i0) / JOIN_WAVES + 1), i = i0 + JOIN_WAVES * min(lane, n - 1);
-      float2 ml = all_ml[place(i)];
-      if (lane >= n) ml = float2{-INFINITY, 0.f};
-      float mx = ml.x;
+  // every fourth of n pieces, from the wave's first on
+  auto add = [&](const float2 *all_ml, const float *all_o, int n, auto place) {
+    for (int i0 = wave; i0 < n; i0 += JOIN_WAVES * JOIN_AHEAD) {
+      float2 ml[JOIN_AHEAD];
+      f32x2 po[JOIN_AHEAD];
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-      mx = fmaxf(mx, m);
-      // a piece without a visible key (reference and sum as at its start) counts for nothing
-      const float f = ml.x == -INFINITY && ml.y == 0.f ? 0.f : fast_exp2(ml.x - mx);
-      float sum = f == 0.f ? 0.f : ml.y * f;
+      for (int j = 0; j < JOIN_AHEAD; ++j) {
+        const int64_t at = place(min(i0 + JOIN_WAVES * j, n - 1));
+        ml[j] = all_ml[at];
+        po[j] = *reinterpret_cast<const f32x2 *>(all_o + at * D + 2 * lane);
+      }
+      float mx = m;
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-      const float keep = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - mx);
+      for (int j = 0; j < JOIN_AHEAD; ++j) {
+        if (i0 + JOIN_WAVES * j >= n) ml[j] = float2{-INFINITY, 0.f};
+        mx = fmaxf(mx, ml[j].x);
+      }
+      const float f = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - mx);
       m = mx;
-      l = l * keep + sum;
-      o *= keep;
-      for (int j0 = 0; j0 < n; j0 += 8) {                              // eight loads in flight
-        f32x2 po[8];
+      l *= f;
+      o *= f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          po[j] = *reinterpret_cast<const f32x2 *>(all_o + place(i0 + JOIN_WAVES * min(j0 + j, n - 1)) * D + 2 * lane);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float fj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), j0 + j));
-          o[0] += fj == 0.f ? 0.f : po[j][0] * fj;                     // lanes behind the last piece hold 0
-          o[1] += fj == 0.f ? 0.f : po[j][1] * fj;
-        }
+      for (int j = 0; j < JOIN_AHEAD; ++j) {
+        // a piece without a visible key (reference and sum as at its start) counts for nothing
+        const bool none = ml[j].x == -INFINITY && ml[j].y == 0.f;
+        const float g = none ? 0.f : fast_exp2(ml[j].x - m);
+        l += none ? 0.f : ml[j].y * g;
+        o[0] += none ? 0.f : po[j][0] * g;
+        o[1] += none ? 0.f : po[j][1] * g;
       }
     }
   };
-  auto join = [&](int t0, int tiles, int in_tile, int segment) {
-    if (tiles <= 0) return;
-    const SegmentPieces p = segment_pieces(t0, t0 + tiles, share);
-    if (p.first == p.last) {
-      if (wave == 0) add(x.piece_ml, x.piece_o, 0, 0, [&](int) { return (int64_t)(2 * x.workers + segment) * x.slot_rows + in_tile; });
-      return;
-    }
-    add(x.piece_ml, x.piece_o, p.first + wave, p.last, [&](int i) { return (int64_t)piece_slot(i, t0, share) * x.slot_rows + in_tile; });
-  };
+  auto join = [&](const PieceList &pieces) { add(x.piece_ml, x.piece_o, pieces.count(), [&](int i) { return pieces.at(i); }); };
   auto common = [&](const SeqWalk &c, int head, int crow) {
-    const int parts = common_parts(c.s2 / COMMON_TILE, x.c_splits);
     const int64_t at = ((int64_t)head * x.c_row_tiles + crow / 256) * x.c_splits;
-    add(x.common_ml, x.common_o, wave, parts - 1, [&](int i) { return (at + i) * 256 + crow % 256; });
+    add(x.common_ml, x.common_o, common_parts(c.s2 / COMMON_TILE, x.c_splits), [&](int i) { return (at + i) * 256 + crow % 256; });
   };
   if (token) {
     if (x.own_common) common(w, seg, row);
-    join(own0, w.tiles, row - rt * tile_rows, x.n_kv * x.p_row_tiles + (b * x.n_kv + kvh) * x.row_tiles + rt);
+    if (w.tiles > 0) join(own);
     if (x.p_cap > 0) {
       const int prow = b * x.rows + row, prt = prow / tile_rows;
       if (x.p_common) common(pw, kvh, prow);
-      join((kvh * x.p_row_tiles + prt) * pw.places() + SEGMENT_COST, pw.tiles, prow - prt * tile_rows, kvh * x.p_row_tiles + prt);
+      if (pw.tiles > 0) {
+        PieceList l = own;
+        l.t0 = (kvh * x.p_row_tiles + prt) * pw.places() + SEGMENT_COST;
+        l.p = segment_pieces(l.t0, l.t0 + pw.tiles, share);
+        l.segment = kvh * x.p_row_tiles + prt;
+        l.base = prow - prt * tile_rows;
+        join(l);
+      }
     }
   }
   __shared__ float sm[JOIN_WAVES], sl[JOIN_WAVES];
@@ -698,33 +824,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   const f32x2 r = {o[0] * inv, o[1] * inv};
   bf16_t *to = x.o + b * x.o_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.o_sh + t * x.o_st;
   *reinterpret_cast<unsigned *>(to + 2 * lane) = __builtin_bit_cast(unsigned, __builtin_convertvector(r, bf16x2));
-  if (x.stat && lane == 0) x.stat[(int64_t)seg * x.rows + row] = float2{m, inv};
-}
-
-// Weight of every slot: the column sums of the softmax, from the logits that the workers left.  A thread takes
-// four slots of a tile (slots and tiles are aligned alike).
-__global__ __launch_bounds__(256) void cache_weight_kernel(CacheCall x) {
-  const int slot = 4 * (blockIdx.x * 256 + threadIdx.x), kvh = blockIdx.y, b = blockIdx.z;
-  const SeqWalk w = walk_of_uniform(x, b);
-  if (slot >= w.len) return;
-  const int tau = w.tile_of(slot);
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  if (tau >= 0) {
-    const int64_t head = (int64_t)b * x.n_kv + kvh;
-    const float *s = x.logits + (head * x.max_tiles + tau) * (x.rows * CACHE_TILE) + (slot - w.base(tau));
-    const float2 *st = x.stat + head * x.rows;
-#pragma unroll 4
-    for (int r = 0; r < x.rows; ++r) {
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(s + r * CACHE_TILE);
-      const float2 ml = st[r];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] += v[i] == -INFINITY ? 0.f : fast_exp2(v[i] - ml.x) * ml.y;
-    }
-  }
-  float *to = x.weight + b * x.w_sb + kvh * x.w_sh + slot;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (slot + i < w.len) to[i] = x.add_weights ? to[i] + sum[i] : sum[i];
+  if (x.stat && lane == 0) x.stat[(int64_t)seg * x.rows + row] = float2{m, l};
 }
 
 // The same for more than 16 rows, whose logits would be more bytes than the keys: they are computed anew.  A wave
@@ -754,7 +854,7 @@ __global__ __launch_bounds__(256) void cache_column_kernel(CacheCall x) {
     const int row = min(r0 + n, x.rows - 1), t = row / x.group;
     const bf16_t *q = x.q + b * x.q_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.q_sh + t * x.q_st + 8 * g;
     const float2 ml = x.stat[head * x.rows + row];
-    const float inv = r0 + n < x.rows ? ml.y : 0.f, m = ml.x == -INFINITY ? 0.f : ml.x;
+    const float inv = r0 + n < x.rows && (ml.y > 0.f || ml.y != ml.y) ? 1.0f / ml.y : 0.f, m = ml.x == -INFINITY ? 0.f : ml.x;
     f32x4 s[4];
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
@@ -1086,13 +1186,10 @@ hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
   if (e != hipSuccess) return e;
   e = x.row_blocks == 1 ? launch_workers<1>(x, st) : launch_workers<2>(x, st);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(cache_join_kernel, dim3(x.batch * x.n_kv * x.rows), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks);
-  if ((e = hipGetLastError()) != hipSuccess || !x.weight) return e;
-  if (!x.logits) {
-    hipLaunchKernelGGL(cache_column_kernel, dim3((x.capacity + COLUMN_KEYS - 1) / COLUMN_KEYS, x.n_kv, x.batch), dim3(256), 0, st, x);
-    return hipGetLastError();
-  }
-  hipLaunchKernelGGL(cache_weight_kernel, dim3((x.capacity + 1023) / 1024, x.n_kv, x.batch), dim3(256), 0, st, x);
+  const int joins = x.batch * x.n_kv * x.rows, weigh = x.logits ? x.batch * x.n_kv * ((x.capacity + 1023) / 1024) : 0;
+  hipLaunchKernelGGL(cache_join_kernel, dim3(joins + weigh), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks, joins);
+  if ((e = hipGetLastError()) != hipSuccess || !x.weight || x.logits) return e;
+  hipLaunchKernelGGL(cache_column_kernel, dim3((x.capacity + COLUMN_KEYS - 1) / COLUMN_KEYS, x.n_kv, x.batch), dim3(256), 0, st, x);
   return hipGetLastError();
 }
 

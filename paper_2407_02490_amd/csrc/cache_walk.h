@@ -70,16 +70,35 @@ MINF_HD int32_t worker_share(int32_t total, int32_t workers) {
   return c < 1 ? 1 : c;
 }
 
-// Workers of the segment (one row tile of one sequence and K/V head) whose tiles lie at the places [t0, t1) of
-// the list: first .. last.  The part that begins at a worker's own first place is its piece 0, another one its
-// piece 1: no worker has more than two parts of segments that it does not hold whole.
+// Workers come in groups (workgroups) of WORKER_GROUP.  The segment (one row tile of one sequence and K/V head)
+// whose tiles lie at the places [t0, t1) of the list is taken by the workers first .. last, and leaves a piece per
+// worker, except that a group whose places all lie in it joins its workers' pieces to one.
+// Slots of the pieces: a part that begins at a worker's own first place takes the worker's slot 0 (so does a
+// group's piece: of its first worker), another one slot 1; no worker has more than two parts of segments that
+// it does not hold whole.
+constexpr int WORKER_GROUP = 4;
+MINF_HD bool group_inside(int32_t group, int32_t t0, int32_t t1, int32_t share) {
+  const int32_t g0 = group * WORKER_GROUP * share;
+  return g0 >= t0 && g0 + WORKER_GROUP * share <= t1;
+}
 struct SegmentPieces {
-  int32_t first, last;
+  int32_t first, last;              // workers
+  int32_t g0, g1;                   // groups that lie inside (g0 >= g1: none)
+  MINF_HD int32_t count() const { return g0 < g1 ? last - first + 1 - (g1 - g0) * (WORKER_GROUP - 1) : last - first + 1; }
+  // worker whose slot holds piece i
+  MINF_HD int32_t worker(int32_t i) const {
+    const int32_t head = g0 * WORKER_GROUP - first;
+    if (g0 >= g1 || i < head) return first + i;
+    return i < head + g1 - g0 ? (g0 + i - head) * WORKER_GROUP : g1 * WORKER_GROUP + i - head - (g1 - g0);
+  }
 };
 MINF_HD SegmentPieces segment_pieces(int32_t t0, int32_t t1, int32_t share) {
   SegmentPieces p;
   p.first = t0 / share;
   p.last = (t1 - 1) / share;
+  const int32_t group_places = WORKER_GROUP * share;
+  p.g0 = (t0 + group_places - 1) / group_places;
+  p.g1 = t1 / group_places;
   return p;
 }
 MINF_HD int32_t piece_slot(int32_t worker, int32_t t0, int32_t share) {

@@ -238,8 +238,8 @@ struct CacheCall {
   float c_log2;
   // workspace
   float *logits;                        // [sequence, K/V head, max_tiles][rows][32], base 2; NULL: not kept
-  float2 *stat;                         // [sequence, K/V head, rows]: maximum, 1 / sum; NULL: no weights
-  float2 *piece_ml;                     // [2 workers + segments][slot_rows]: maximum, sum
+  float2 *stat;                         // [sequence, K/V head, rows]: reference, sum; NULL: no weights
+  float2 *piece_ml;                     // [2 workers + segments][slot_rows]: reference, sum
   float *piece_o;                       // [2 workers + segments][slot_rows][128]
   float2 *common_ml;                    // [K/V head (of a sequence), c_row_tiles][c_splits][256]
   float *common_o;                      // [K/V head (of a sequence), c_row_tiles][c_splits][256][128]

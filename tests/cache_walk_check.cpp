@@ -92,18 +92,24 @@ static int shares() {
           if (t == 0) continue;
           t0 += SEGMENT_COST;
           const SegmentPieces p = segment_pieces(t0, t0 + t, share);
-          CHECK(p.first >= 0 && p.last < workers && p.first <= p.last);
+          CHECK(p.first >= 0 && p.last < workers && p.first <= p.last && p.count() >= 1);
           if (p.first != p.last) {
-            int covered = 0;
-            for (int w = p.first; w <= p.last; ++w) {
-              const int a = t0 > w * share ? t0 : w * share, b = t0 + t < (w + 1) * share ? t0 + t : (w + 1) * share;
-              CHECK(b > a);
-              covered += b - a;
+            // every worker of the segment is covered by one piece, its own or its group's, in ascending order
+            std::set<int> seen;
+            int before = -1;
+            for (int i = 0; i < p.count(); ++i) {
+              const int w = p.worker(i);
+              CHECK(w > before && w >= p.first && w <= p.last);
+              before = w;
+              const bool whole = group_inside(w / WORKER_GROUP, t0, t0 + t, share);
+              CHECK(!whole || w % WORKER_GROUP == 0);
+              for (int k = 0; k < (whole ? WORKER_GROUP : 1); ++k) CHECK(seen.insert(w + k).second);
+              const int a = t0 > w * share ? t0 : w * share;
               const int slot = piece_slot(w, t0, share);
               CHECK(slot == 2 * w + (a > w * share));      // as the worker numbers it
               CHECK(used.insert(slot).second);
             }
-            CHECK(covered == t);
+            CHECK((int)seen.size() == p.last - p.first + 1 && *seen.begin() == p.first && *seen.rbegin() == p.last);
           }
           t0 += t;
         }

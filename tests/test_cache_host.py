@@ -178,12 +178,12 @@ def test_binding_checks_its_tensors():
     from paper_2407_02490_amd import binding as B
     k = torch.zeros(2, 2, 64, 128, dtype=torch.bfloat16)
     lens = torch.zeros(2, dtype=torch.int32)
-    B.KVCache(k, k, lens, torch.zeros(2, 2, 64)).c_struct()
+    assert B.KVCache(k, k, lens, torch.zeros(2, 2, 64)).c_struct().capacity == 64
     for bad in ((k.float(), k, lens, None), (k, k[:, :, :32], lens, None), (k, k, lens.long(), None), (k, k, lens[:1], None),
                 (k, k, lens, torch.zeros(2, 2, 63)), (k, k, lens, torch.zeros(2, 2, 64).double()),
                 (k, k, lens, torch.zeros(2, 64, 2).transpose(1, 2)), (k.transpose(2, 3), k.transpose(2, 3), lens, None)):
         with pytest.raises(AssertionError):
-            B.KVCache(*bad).c_struct()
+            B.KVCache(*bad)
     c = B.KVCache(k, k, lens)
     q = torch.zeros(2, 4, 1, 128, dtype=torch.bfloat16)
     assert B.minf_cache_attn_workspace_bytes(q, c) > 0
