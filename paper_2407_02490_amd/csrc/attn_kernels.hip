@@ -766,7 +766,11 @@ struct AllCls {
 //    infinite reference.  The body is one straight path, which keeps the 128
 //    output accumulators in place; the first iteration has no output update,
 //    the last two form logits nobody consumes.
-template <class Cls>
+//  - AHEAD = 1 issues the loads of an iteration one tile further ahead, K(t+4) and V(t+2), into the slots that are
+//    free behind the barrier, and waits for those of two iterations ago: the cache calls, whose tiles come from
+//    memory rather than from the caches, one pass over them (half an iteration is too short for that: 8 K/V
+//    heads of 128K tokens, 128 rows, 124 us at AHEAD = 0).
+template <class Cls, int AHEAD = 0>
 struct AshapeLoop {
   WaveState &st;
   const QAcc &qa;
@@ -786,6 +790,7 @@ struct AshapeLoop {
   static constexpr unsigned k_slot(int i) { return (unsigned)(i & 3) * TILE_BYTES; }
   static constexpr unsigned v_slot(int i) { return (unsigned)(4 + (i & 3)) * TILE_BYTES; }
   int kb1, kb2, kb3, ti3;    // key bases of tiles t+1, t+2, t+3 (indices clamped to T-1); index of the last
+  int kb4 = 0;               // AHEAD: of tile t+4 (ti3: its index)
   int cls_cur;
   bool &has_ref;
 
@@ -797,8 +802,8 @@ struct AshapeLoop {
 
   // for iteration t, from the tile state of iteration t
   __device__ inline void prepare(int t) {
-    kt_ = d.kw + (size_t)kb3 * d.k_rb;                                  // K(t+3) -> slot (t+3) mod 4
-    vt_ = d.vw + (size_t)kb1 * d.v_rb;                                  // V(t+1) -> slot (t+1) mod 4
+    kt_ = d.kw + (size_t)(AHEAD ? kb4 : kb3) * d.k_rb;                  // K(t+3) -> slot (t+3) mod 4
+    vt_ = d.vw + (size_t)(AHEAD ? kb2 : kb1) * d.v_rb;                  // V(t+1) -> slot (t+1) mod 4
     cls_nxt_ = t + 1 < T ? cls.of(kb1) : 0;
   }
 
@@ -837,16 +842,18 @@ struct AshapeLoop {
     }
     // the iteration's scalar operands were prepared during the previous one
     const char *kt = kt_, *vt = vt_;
-    const unsigned k_dst = lds_addr_of(lds) + k_slot(PH + 3) + d.lds_w;
-    const unsigned v_dst = lds_addr_of(lds) + v_slot(PH + 1) + d.lds_w;
+    const unsigned k_dst = lds_addr_of(lds) + k_slot(PH + 3 + AHEAD) + d.lds_w;
+    const unsigned v_dst = lds_addr_of(lds) + v_slot(PH + 1 + AHEAD) + d.lds_w;
     const int cls_nxt = cls_nxt_, kb_nxt = kb1;
     const bool attend_cur = cls_cur != 0;
     // ... and the next one's are prepared in round 5, between MFMAs
     auto prepare_next = [&]() {
       kb1 = kb2; kb2 = kb3;
+      if (AHEAD) kb3 = kb4;
+      int &last = AHEAD ? kb4 : kb3;
       if (ti3 + 1 < T) {
         ++ti3;
-        kb3 = ti3 == T1 ? s2 : kb3 + BK;
+        last = ti3 == T1 ? s2 : last + BK;
       }
       prepare(t + 1);
     };
@@ -934,8 +941,9 @@ struct AshapeLoop {
         // The iteration's one barrier sits in its middle.  Landed and visible behind it: the loads
         // issued in rounds 4..7 of the iteration before, K(t+2) and V(t), which the next iteration
         // reads.  Free behind it: the slots this iteration's loads (rounds 4..7) overwrite, which
-        // held K(t-1) and V(t-3), last read two and three iterations ago.
-        MINF_WAIT_VMCNT(0);
+        // held K(t-1) and V(t-3), last read two and three iterations ago.  (AHEAD: landed the loads of the
+        // iteration before that; free K(t) and V(t-2), last read in the iteration before.)
+        if (AHEAD) MINF_WAIT_VMCNT(8); else MINF_WAIT_VMCNT(0);
         __syncthreads();
       }
     };
@@ -967,6 +975,7 @@ struct AshapeLoop {
 // iteration has no output update.  (Loads behind Q and a zero update: windows of (0, 64) 333 us instead of
 // 323, (128, 1024) 714 instead of 705, 8 heads of 128K tokens; longer ones the same.)  In vs_share_kernel Q
 // is there and a pass does start on K(0) alone.
+template <int AHEAD = 0>
 __device__ inline void ashape_first_loads(const AshapeCtx &c, const WaveDma &d) {
   const unsigned dst = lds_addr_of(c.lds) + d.lds_w;
   auto tile = [&](const char *w, unsigned rb, const DmaRows &rows, int t, unsigned to) {
@@ -978,21 +987,26 @@ __device__ inline void ashape_first_loads(const AshapeCtx &c, const WaveDma &d) 
   tile(d.kw, d.k_rb, d.k, 1, dst + TILE_BYTES);
   tile(d.vw, d.v_rb, d.v, 0, dst + 4 * TILE_BYTES);
   tile(d.kw, d.k_rb, d.k, 2, dst + 2 * TILE_BYTES);
+  if (AHEAD) {
+    tile(d.kw, d.k_rb, d.k, 3, dst + 3 * TILE_BYTES);
+    tile(d.vw, d.v_rb, d.v, 1, dst + 5 * TILE_BYTES);
+  }
 }
 
 // After ashape_first_loads.
-template <class Cls>
+template <class Cls, int AHEAD = 0>
 __device__ inline void ashape_pass_pipelined(const AshapeCtx &c, const WaveDma &d, WaveState &st, const QAcc &qa,
                                              bool &has_ref, const LaneOfs &lo, const MaskP &mp, const Cls &cls,
                                              int lane) {
-  AshapeLoop<Cls> lp{st, qa, lo, mp, d, cls, c.c_log2, lane, c.T, c.T1, c.s2, c.lds, 0, 0, 0, 0, 0, has_ref};
+  AshapeLoop<Cls, AHEAD> lp{st, qa, lo, mp, d, cls, c.c_log2, lane, c.T, c.T1, c.s2, c.lds, 0, 0, 0, 0, 0, 0, has_ref};
   const int last = c.T - 1;
   const int kb0 = lp.tile_base(0);
   lp.kb1 = lp.tile_base(min(1, last)); lp.kb2 = lp.tile_base(min(2, last));
   lp.ti3 = min(3, last); lp.kb3 = lp.tile_base(lp.ti3);
+  if (AHEAD) { lp.ti3 = min(4, last); lp.kb4 = lp.tile_base(lp.ti3); }
   f32x16 sa[2][2], sb[2][2];
   bf16x8 pa[2][2][2], pb[2][2][2];
-  MINF_WAIT_VMCNT(12);      // K(0)
+  if (AHEAD) MINF_WAIT_VMCNT(20); else MINF_WAIT_VMCNT(12);      // K(0)
   __syncthreads();
   lp.cls_cur = lp.cls.of(kb0);
   // also for a tile this wave does not attend: its (finite) logits are turned into P = 0
@@ -1002,10 +1016,10 @@ __device__ inline void ashape_pass_pipelined(const AshapeCtx &c, const WaveDma &
     if (!has_ref) take_reference<2>(sa, st, c.c_log2);
     has_ref = true;
   }
-  MINF_WAIT_VMCNT(4);       // K(1), V(0); K(2) is awaited at the barrier of iteration 0
+  if (AHEAD) MINF_WAIT_VMCNT(12); else MINF_WAIT_VMCNT(4);       // K(1), V(0); K(2) is awaited at the barrier of iteration 0
   __syncthreads();          // all waves are done with K(0)
   lp.prepare(0);
-  typename AshapeLoop<Cls>::Lead lead;
+  typename AshapeLoop<Cls, AHEAD>::Lead lead;
   lp.template read_lead<0, true>(lead);
   // iterations t = 0 .. T (the last one finishes the output update of tile T-1; an update alone behind
   // the loop makes the compiler spill); T is the same for the four waves, which meet at the barrier of
@@ -2948,7 +2962,7 @@ __global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
   d.kw = reinterpret_cast<const char *>(c.kh) + (size_t)(16 * wave) * d.k_rb;
   d.vw = reinterpret_cast<const char *>(c.vh) + (size_t)(16 * wave) * d.v_rb;
   d.lds_w = wave * 4096;
-  ashape_first_loads(c, d);
+  ashape_first_loads<1>(c, d);
 
   WaveState st;
   auto load_rows = [&]() {
@@ -2980,7 +2994,7 @@ __global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
   QAcc qa;
   pin_q(qa, st);
   bool has_ref = false;
-  ashape_pass_pipelined<AllCls>(c, d, st, qa, has_ref, lo, mp, AllCls(), lane);
+  ashape_pass_pipelined<AllCls, 1>(c, d, st, qa, has_ref, lo, mp, AllCls(), lane);
   if (__syncthreads_or(needs_exact(st) ? 1 : 0)) {
     load_rows();
     reset_for_max_pass(st);

@@ -651,9 +651,9 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
 }
 
 // ---- joining the pieces ---------------------------------------------------------------------------------
-// One workgroup per output row: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the pieces of the row's
-// own segment, of the prefix's and of the common slots.  A wave takes every fourth piece, eight at a time with all
-// their loads in flight.  Rows without a visible key, or without a token, give zeros.
+// o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the pieces of the row's
+// own segment, of the prefix's and of the common slots.  Four waves share a row (W = 4: every fourth piece each) or, of
+// many rows, each wave takes one (W = 1); eight pieces at a time with all their loads in flight.  Rows without a visible key, or without a token, give zeros.
 // Further workgroups give the slots their weights (where the logits were kept): they need the references and sums
 // of a K/V head's rows, which they join themselves, rather than wait for another launch.
 constexpr int JOIN_WAVES = 4, JOIN_AHEAD = 8;
@@ -671,11 +671,14 @@ struct PieceList {
   }
 };
 
+template <int W>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x, int tile_rows, int joins) {
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   const bool joining = (int)blockIdx.x < joins;
   // joining: the row of a K/V head of a sequence; else 1024 slots of one
-  const int per_head = joining ? x.rows : (x.capacity + 1023) / 1024, id = joining ? blockIdx.x : blockIdx.x - joins;
+  const int per_head = joining ? x.rows : (x.capacity + 1023) / 1024;
+  const int id = !joining ? blockIdx.x - joins : W == 4 ? blockIdx.x : blockIdx.x * JOIN_WAVES + wave;
+  if (joining && W == 1 && id >= x.batch * x.n_kv * x.rows) return;
   const int seg = id / per_head, item = id - seg * per_head;
   const int b = seg / x.n_kv, kvh = seg - b * x.n_kv;
   const int mine = first_lens(x, lane);
@@ -751,19 +754,19 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   f32x2 o = {0.f, 0.f};
   // every fourth of n pieces, from the wave's first on
   auto add = [&](const float2 *all_ml, const float *all_o, int n, auto place) {
-    for (int i0 = wave; i0 < n; i0 += JOIN_WAVES * JOIN_AHEAD) {
+    for (int i0 = W == 4 ? wave : 0; i0 < n; i0 += W * JOIN_AHEAD) {
       float2 ml[JOIN_AHEAD];
       f32x2 po[JOIN_AHEAD];
 #pragma unroll
       for (int j = 0; j < JOIN_AHEAD; ++j) {
-        const int64_t at = place(min(i0 + JOIN_WAVES * j, n - 1));
+        const int64_t at = place(min(i0 + W * j, n - 1));
         ml[j] = all_ml[at];
         po[j] = *reinterpret_cast<const f32x2 *>(all_o + at * D + 2 * lane);
       }
       float mx = m;
 #pragma unroll
       for (int j = 0; j < JOIN_AHEAD; ++j) {
-        if (i0 + JOIN_WAVES * j >= n) ml[j] = float2{-INFINITY, 0.f};
+        if (i0 + W * j >= n) ml[j] = float2{-INFINITY, 0.f};
         mx = fmaxf(mx, ml[j].x);
       }
       const float f = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - mx);
@@ -802,23 +805,25 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
       }
     }
   }
-  __shared__ float sm[JOIN_WAVES], sl[JOIN_WAVES];
-  __shared__ f32x2 so[JOIN_WAVES][64];
-  if (lane == 0) { sm[wave] = m; sl[wave] = l; }
-  so[wave][lane] = o;
-  __syncthreads();
-  if (wave != 0) return;
-  m = -INFINITY; l = 0.f;
-  o = f32x2{0.f, 0.f};
+  if (W == 4) {
+    __shared__ float sm[JOIN_WAVES], sl[JOIN_WAVES];
+    __shared__ f32x2 so[JOIN_WAVES][64];
+    if (lane == 0) { sm[wave] = m; sl[wave] = l; }
+    so[wave][lane] = o;
+    __syncthreads();
+    if (wave != 0) return;
+    m = -INFINITY; l = 0.f;
+    o = f32x2{0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < JOIN_WAVES; ++i) m = fmaxf(m, sm[i]);
+    for (int i = 0; i < JOIN_WAVES; ++i) m = fmaxf(m, sm[i]);
 #pragma unroll
-  for (int i = 0; i < JOIN_WAVES; ++i) {
-    if (sm[i] == -INFINITY && sl[i] == 0.f) continue;
-    const float f = fast_exp2(sm[i] - m);
-    l += sl[i] * f;
-    o[0] += so[i][lane][0] * f;
-    o[1] += so[i][lane][1] * f;
+    for (int i = 0; i < JOIN_WAVES; ++i) {
+      if (sm[i] == -INFINITY && sl[i] == 0.f) continue;
+      const float f = fast_exp2(sm[i] - m);
+      l += sl[i] * f;
+      o[0] += so[i][lane][0] * f;
+      o[1] += so[i][lane][1] * f;
+    }
   }
   const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
   const f32x2 r = {o[0] * inv, o[1] * inv};
@@ -850,26 +855,45 @@ __global__ __launch_bounds__(256) void cache_column_kernel(CacheCall x) {
   float sum[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+  struct Block {                                                // this lane's row of 16
+    bf16x8 q[4];
+    float2 ml;
+    int t;
+  };
+  auto load = [&](int r0, Block &w) {
+    const int row = min(r0 + n, x.rows - 1);
+    w.t = row / x.group;
+    const bf16_t *q = x.q + b * x.q_sb + (int64_t)(kvh * x.group + row - w.t * x.group) * x.q_sh + w.t * x.q_st + 8 * g;
+    w.ml = x.stat[head * x.rows + row];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) w.q[ks] = *reinterpret_cast<const bf16x8 *>(q + 32 * ks);
+  };
+  Block ahead;
+  load(0, ahead);
   for (int r0 = 0; r0 < x.rows && !hidden; r0 += 16) {
-    const int row = min(r0 + n, x.rows - 1), t = row / x.group;
-    const bf16_t *q = x.q + b * x.q_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.q_sh + t * x.q_st + 8 * g;
-    const float2 ml = x.stat[head * x.rows + row];
-    const float inv = r0 + n < x.rows && (ml.y > 0.f || ml.y != ml.y) ? 1.0f / ml.y : 0.f, m = ml.x == -INFINITY ? 0.f : ml.x;
+    const Block w = ahead;
+    if (r0 + 16 < x.rows) load(r0 + 16, ahead);
+    const int t = w.t;
+    const float inv = r0 + n < x.rows && (w.ml.y > 0.f || w.ml.y != w.ml.y) ? 1.0f / w.ml.y : 0.f;
+    const float m = w.ml.x == -INFINITY ? 0.f : w.ml.x;
     f32x4 s[4];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      const bf16x8 qf = *reinterpret_cast<const bf16x8 *>(q + 32 * ks);
+    for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][ks], qf, ks == 0 ? zero : s[kt], 0, 0, 0);
+        s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][ks], w.q[ks], ks == 0 ? zero : s[kt], 0, 0, 0);
       }
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i] += inv != 0.f ? fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -m)) * inv : 0.f;
+      continue;
     }
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool sees = whole || cache_visible(kb + 16 * kt + 4 * g + i, i0 + t, x.n_init, x.n_local);
+        const bool sees = cache_visible(kb + 16 * kt + 4 * g + i, i0 + t, x.n_init, x.n_local);
         const float p = fast_exp2(fmaf(s[kt][i], x.c_log2, -m)) * inv;
         sum[4 * kt + i] += sees && inv != 0.f ? p : 0.f;
       }
@@ -896,7 +920,7 @@ __device__ inline unsigned weight_key(float v) {
 }
 
 constexpr int SELECT_THREADS = 1024, SELECT_WAVES = SELECT_THREADS / 64;
-constexpr int SELECT_BINS = 2048, SELECT_COPIES = 4;
+constexpr int SELECT_BINS = 2048, SELECT_COPIES = 4, SELECT_AHEAD = 8;   // AHEAD: loads in flight a lane
 // The kept weight of rank `want` is found digit by digit: 11, 11 and 10 bits from the most significant one.
 __device__ constexpr int select_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
 __device__ constexpr int select_bins(int pass) { return pass == 2 ? 1024 : 2048; }
@@ -948,10 +972,16 @@ __device__ inline void select_count(const SelectRow &r, int from, int to, unsign
   __syncthreads();
   from = max(from, r.first);
   to = min(to, r.last);
-#pragma unroll 4
-  for (int i = from + tid; i < to; i += SELECT_THREADS) {
-    const unsigned k = weight_key(r.w[i]);
-    if ((k & select_mask(PASS)) == prefix) atomicAdd(&s.hist[tid & (SELECT_COPIES - 1)][(k >> select_shift(PASS)) & (select_bins(PASS) - 1)], 1);
+  for (int i0 = from; i0 < to; i0 += SELECT_AHEAD * SELECT_THREADS) {
+    float v[SELECT_AHEAD];
+#pragma unroll
+    for (int j = 0; j < SELECT_AHEAD; ++j) v[j] = r.w[min(i0 + j * SELECT_THREADS + tid, to - 1)];
+#pragma unroll
+    for (int j = 0; j < SELECT_AHEAD; ++j) {
+      const unsigned k = weight_key(v[j]);
+      if (i0 + j * SELECT_THREADS + tid < to && (k & select_mask(PASS)) == prefix)
+        atomicAdd(&s.hist[tid & (SELECT_COPIES - 1)][(k >> select_shift(PASS)) & (select_bins(PASS) - 1)], 1);
+    }
   }
   __syncthreads();
 }
@@ -986,30 +1016,42 @@ __device__ inline void select_emit(const SelectRow &r, int from, int to, unsigne
   const int per = (to - from + SELECT_THREADS - 1) / SELECT_THREADS * 64;
   const int w0 = from + wave * per, w1 = min(w0 + per, min(to, r.last));
   const unsigned long long below = (1ull << lane) - 1;
-  auto look = [&](int i, unsigned long long &g, unsigned long long &e) {
-    const bool in = i >= r.first && i < w1;
-    const unsigned k = in ? weight_key(r.w[i]) : 0u;
-    g = __builtin_amdgcn_ballot_w64(in && k > key);
-    e = __builtin_amdgcn_ballot_w64(in && k == key);
+  // keys of SELECT_AHEAD * 64 slots from i0 on, with their loads in flight
+  auto look = [&](int i0, unsigned (&k)[SELECT_AHEAD]) {
+    float v[SELECT_AHEAD];
+#pragma unroll
+    for (int j = 0; j < SELECT_AHEAD; ++j) v[j] = r.w[min(i0 + 64 * j + lane, w1 - 1)];
+#pragma unroll
+    for (int j = 0; j < SELECT_AHEAD; ++j) k[j] = weight_key(v[j]);
   };
+  auto in = [&](int i) { return i >= r.first && i < w1; };
   int ng = 0, ne = 0;
-  for (int i0 = w0; i0 < w1; i0 += 64) {
-    unsigned long long g, e;
-    look(i0 + lane, g, e);
-    ng += __popcll(g);
-    ne += __popcll(e);
+  for (int i0 = w0; i0 < w1; i0 += 64 * SELECT_AHEAD) {
+    unsigned k[SELECT_AHEAD];
+    look(i0, k);
+#pragma unroll
+    for (int j = 0; j < SELECT_AHEAD; ++j) {
+      const bool here = in(i0 + 64 * j + lane);
+      ng += __popcll(__builtin_amdgcn_ballot_w64(here && k[j] > key));
+      ne += __popcll(__builtin_amdgcn_ballot_w64(here && k[j] == key));
+    }
   }
   int all;
   const int before_g = block_scan(lane == 0 ? ng : 0, s.part, all), before_e = block_scan(lane == 0 ? ne : 0, s.part, all);
   gt += uni(before_g);
   eq += uni(before_e);
-  for (int i0 = w0; i0 < w1; i0 += 64) {
-    unsigned long long g, e;
-    look(i0 + lane, g, e);
-    const int gr = gt + __popcll(g & below), er = eq + __popcll(e & below);
-    if ((g >> lane) & 1 || ((e >> lane) & 1 && er < want)) kept[r.first + gr + min(er, want)] = i0 + lane;
-    gt += __popcll(g);
-    eq += __popcll(e);
+  for (int i0 = w0; i0 < w1; i0 += 64 * SELECT_AHEAD) {
+    unsigned k[SELECT_AHEAD];
+    look(i0, k);
+#pragma unroll
+    for (int j = 0; j < SELECT_AHEAD; ++j) {
+      const int i = i0 + 64 * j + lane;
+      const unsigned long long g = __builtin_amdgcn_ballot_w64(in(i) && k[j] > key), e = __builtin_amdgcn_ballot_w64(in(i) && k[j] == key);
+      const int gr = gt + __popcll(g & below), er = eq + __popcll(e & below);
+      if ((g >> lane) & 1 || ((e >> lane) & 1 && er < want)) kept[r.first + gr + min(er, want)] = i;
+      gt += __popcll(g);
+      eq += __popcll(e);
+    }
   }
   // the first and the last slots stay whatever they weigh
   for (int i = from + tid; i < min(to, r.first); i += SELECT_THREADS) kept[i] = i;
@@ -1186,8 +1228,14 @@ hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
   if (e != hipSuccess) return e;
   e = x.row_blocks == 1 ? launch_workers<1>(x, st) : launch_workers<2>(x, st);
   if (e != hipSuccess) return e;
-  const int joins = x.batch * x.n_kv * x.rows, weigh = x.logits ? x.batch * x.n_kv * ((x.capacity + 1023) / 1024) : 0;
-  hipLaunchKernelGGL(cache_join_kernel, dim3(joins + weigh), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks, joins);
+  // Four waves per row while that is a round of the chip's waves or less
+  const int rows = x.batch * x.n_kv * x.rows, weigh = x.logits ? x.batch * x.n_kv * ((x.capacity + 1023) / 1024) : 0;
+  if (rows <= 1024) {
+    hipLaunchKernelGGL(cache_join_kernel<4>, dim3(rows + weigh), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks, rows);
+  } else {
+    const int joins = (rows + JOIN_WAVES - 1) / JOIN_WAVES;
+    hipLaunchKernelGGL(cache_join_kernel<1>, dim3(joins + weigh), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks, joins);
+  }
   if ((e = hipGetLastError()) != hipSuccess || !x.weight || x.logits) return e;
   hipLaunchKernelGGL(cache_column_kernel, dim3((x.capacity + COLUMN_KEYS - 1) / COLUMN_KEYS, x.n_kv, x.batch), dim3(256), 0, st, x);
   return hipGetLastError();
