@@ -836,7 +836,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
 // takes 64 keys (K as A operands, in registers) and all rows, 16 at a time; per row block 16 MFMAs and 16
 // exponentials a lane.
 constexpr int COLUMN_KEYS = 256;                                // per workgroup
-__global__ __launch_bounds__(256) void cache_column_kernel(CacheCall x) {
+__global__ __launch_bounds__(256, 3) void cache_column_kernel(CacheCall x) {
   const int kvh = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4, kb = blockIdx.x * COLUMN_KEYS + wave * 64;
   const int len = uni(min(max(x.lens[b], 0), x.capacity)), i0 = len - x.n_new;
@@ -874,8 +874,9 @@ __global__ __launch_bounds__(256) void cache_column_kernel(CacheCall x) {
     const Block w = ahead;
     if (r0 + 16 < x.rows) load(r0 + 16, ahead);
     const int t = w.t;
-    const float inv = r0 + n < x.rows && (w.ml.y > 0.f || w.ml.y != w.ml.y) ? 1.0f / w.ml.y : 0.f;
-    const float m = w.ml.x == -INFINITY ? 0.f : w.ml.x;
+    // p = 2^(c s - m) / l = 2^(c s - (m + log2 l)); a row without a key, or behind the last: 2^-inf
+    const bool none = r0 + n >= x.rows || (w.ml.x == -INFINITY && w.ml.y == 0.f);
+    const float m = none ? INFINITY : w.ml.x + __builtin_amdgcn_logf(w.ml.y);
     f32x4 s[4];
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks)
@@ -886,7 +887,7 @@ __global__ __launch_bounds__(256) void cache_column_kernel(CacheCall x) {
       }
     if (whole) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i] += inv != 0.f ? fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -m)) * inv : 0.f;
+      for (int i = 0; i < 16; ++i) sum[i] += fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -m));
       continue;
     }
 #pragma unroll
@@ -894,8 +895,8 @@ __global__ __launch_bounds__(256) void cache_column_kernel(CacheCall x) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const bool sees = cache_visible(kb + 16 * kt + 4 * g + i, i0 + t, x.n_init, x.n_local);
-        const float p = fast_exp2(fmaf(s[kt][i], x.c_log2, -m)) * inv;
-        sum[4 * kt + i] += sees && inv != 0.f ? p : 0.f;
+        const float p = fast_exp2(fmaf(s[kt][i], x.c_log2, -m));
+        sum[4 * kt + i] += sees ? p : 0.f;
       }
   }
 #pragma unroll
@@ -1025,28 +1026,34 @@ __device__ inline void select_emit(const SelectRow &r, int from, int to, unsigne
     for (int j = 0; j < SELECT_AHEAD; ++j) k[j] = weight_key(v[j]);
   };
   auto in = [&](int i) { return i >= r.first && i < w1; };
+  // a wave's keys stay in registers between the counting and the writing
+  constexpr int BATCH = 64 * SELECT_AHEAD, BATCHES = 32768 / SELECT_THREADS / SELECT_AHEAD;
+  unsigned k[BATCHES][SELECT_AHEAD];
   int ng = 0, ne = 0;
-  for (int i0 = w0; i0 < w1; i0 += 64 * SELECT_AHEAD) {
-    unsigned k[SELECT_AHEAD];
-    look(i0, k);
+#pragma unroll
+  for (int t = 0; t < BATCHES; ++t) {
+    const int i0 = w0 + t * BATCH;
+    if (i0 >= w1) break;
+    look(i0, k[t]);
 #pragma unroll
     for (int j = 0; j < SELECT_AHEAD; ++j) {
       const bool here = in(i0 + 64 * j + lane);
-      ng += __popcll(__builtin_amdgcn_ballot_w64(here && k[j] > key));
-      ne += __popcll(__builtin_amdgcn_ballot_w64(here && k[j] == key));
+      ng += __popcll(__builtin_amdgcn_ballot_w64(here && k[t][j] > key));
+      ne += __popcll(__builtin_amdgcn_ballot_w64(here && k[t][j] == key));
     }
   }
   int all;
   const int before_g = block_scan(lane == 0 ? ng : 0, s.part, all), before_e = block_scan(lane == 0 ? ne : 0, s.part, all);
   gt += uni(before_g);
   eq += uni(before_e);
-  for (int i0 = w0; i0 < w1; i0 += 64 * SELECT_AHEAD) {
-    unsigned k[SELECT_AHEAD];
-    look(i0, k);
+#pragma unroll
+  for (int t = 0; t < BATCHES; ++t) {
+    const int i0 = w0 + t * BATCH;
+    if (i0 >= w1) break;
 #pragma unroll
     for (int j = 0; j < SELECT_AHEAD; ++j) {
       const int i = i0 + 64 * j + lane;
-      const unsigned long long g = __builtin_amdgcn_ballot_w64(in(i) && k[j] > key), e = __builtin_amdgcn_ballot_w64(in(i) && k[j] == key);
+      const unsigned long long g = __builtin_amdgcn_ballot_w64(in(i) && k[t][j] > key), e = __builtin_amdgcn_ballot_w64(in(i) && k[t][j] == key);
       const int gr = gt + __popcll(g & below), er = eq + __popcll(e & below);
       if ((g >> lane) & 1 || ((e >> lane) & 1 && er < want)) kept[r.first + gr + min(er, want)] = i;
       gt += __popcll(g);
