@@ -155,11 +155,12 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   p.at_common = p.at_common_ml = p.at_stat = p.at_ml + up(slots * sizeof(float2));
   if (x.p_common || x.own_common) {
     x.c_rows = (int32_t)(prefix ? p_rows : x.rows);
-    x.c_row_tiles = (x.c_rows + 255) / 256;
+    x.c_tile_rows = x.c_rows <= 64 ? 64 : x.c_rows <= 128 ? 128 : 256;
+    x.c_row_tiles = (x.c_rows + x.c_tile_rows - 1) / x.c_tile_rows;
     const int64_t items = (int64_t)(prefix ? 1 : x.batch) * x.n_kv * x.c_row_tiles;
     x.c_splits = common_splits(items, (prefix ? prefix->capacity : x.capacity) / COMMON_TILE);
     if ((items + 8) * x.c_splits > MAX_BLOCKS) return MINF_ERR_SHAPE;
-    const size_t rows = (size_t)items * x.c_splits * 256;
+    const size_t rows = (size_t)items * x.c_splits * x.c_tile_rows;
     p.at_common_ml = p.at_common + up(rows * 128 * sizeof(float));
     p.at_stat = p.at_common_ml + up(rows * sizeof(float2));
   }

@@ -503,18 +503,19 @@ struct CacheSource {
     kh = reinterpret_cast<const char *>(c.prefix ? x.pk + c.kvh * x.pk_sh : x.k + c.b * x.k_sb + c.kvh * x.k_sh);
     vh = reinterpret_cast<const char *>(c.prefix ? x.pv + c.kvh * x.pv_sh : x.v + c.b * x.v_sb + c.kvh * x.v_sh);
   }
+  // 16 rows from row0 on to the LDS address lds
+  __device__ static inline void rows16(const char *row0, const unsigned (&ofs)[4], unsigned lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %0, %1\n\t"
+                 "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
+                 "global_load_lds_dwordx4 %5, %1 offset:3072"
+                 :: "v"(ofs[0]), "s"(row0), "s"(lds), "v"(ofs[1]), "v"(ofs[2]), "v"(ofs[3]) : "memory");
+  }
   // 32 rows from kb on into the tile at lds
   __device__ static inline void tile(const char *h, unsigned rb, const unsigned (&ofs)[4], int kb, unsigned lds) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const char *row0 = h + (uint64_t)(unsigned)(kb + 16 * half) * rb;
-      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\t"
-                   "global_load_lds_dwordx4 %0, %1\n\t"
-                   "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                   "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
-                   "global_load_lds_dwordx4 %5, %1 offset:3072"
-                   :: "v"(ofs[0]), "s"(row0), "s"(lds + 4096 * half), "v"(ofs[1]), "v"(ofs[2]), "v"(ofs[3]) : "memory");
-    }
+    for (int half = 0; half < 2; ++half) rows16(h + (uint64_t)(unsigned)(kb + 16 * half) * rb, ofs, lds + 4096 * half);
   }
   // ... row by row: slots that no row of the call sees are replaced by one that some row does
   __device__ static inline void tile_in_part(const char *h, unsigned rb, int kb, const SeqWalk &w, unsigned lds, int lane) {
@@ -647,6 +648,138 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
     g += cur.t1 - cur.t0 + SEGMENT_COST;
     st.q = q;
     cur = nxt;
+  }
+}
+
+// ---- the slots that 33 to 128 rows see --------------------------------------------------------------------
+// Four waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile) and take 16 NB
+// rows each.  Memory bounds it still: 32 KiB a tile take a CU 1.4 us, the rows 0.5 (NB = 1) to 1.0 us.  (The 256-row
+// kernel, whose waves take 64 rows, runs 1.65 us a tile for any number of rows: 128 rows, 8 heads of 128K tokens,
+// 142 us.)  P in one bf16, as there: the matrix cores have no time to spare for its rest.
+// Order of the workgroups and layout of the results: as cache_common_kernel.
+template <int NB>
+__global__ __launch_bounds__(64 * CACHE_WAVES) void cache_shared_kernel(CacheCall x) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
+  const int per_xcd = blockIdx.x >> 3, rt = per_xcd % x.c_row_tiles;
+  const int group = (per_xcd / x.c_row_tiles) * 8 + (blockIdx.x & 7);          // (K/V head of a sequence, part of the slots)
+  const int heads = (x.p_common ? 1 : x.batch) * x.n_kv;
+  if (group >= heads * x.c_splits) return;
+  const int head = group / x.c_splits, part = group - head * x.c_splits;
+  CachePart c;
+  c.prefix = x.p_common;
+  c.b = c.prefix ? 0 : head / x.n_kv;
+  c.kvh = head - c.b * x.n_kv;
+  c.rt = rt * CACHE_WAVES + wave;                                              // row tile of 16 NB rows
+  const int len = uni(c.prefix ? x.p_lens[0] : x.lens[c.b]);
+  const int tiles = common_slots(min(max(len, 0), c.prefix ? x.p_cap : x.capacity) - (c.prefix ? 1 : x.n_new)) / COMMON_TILE;
+  const int per = common_share(tiles, x.c_splits), t0 = part * per, n = min(per, tiles - t0);
+  if (n <= 0) return;
+
+  CacheSource src;
+  src.strides(x, c.prefix, lane);
+  src.heads(x, c);
+  const unsigned ring = uni(lds_addr_of(lds)) + 4096 * wave;
+  auto fetch = [&](int t) {                                                    // this wave's 16 rows of K and V
+    const unsigned to = ring + (t & 3) * (2 * TILE_BYTES);
+    const int row = (t0 + min(t, n - 1)) * COMMON_TILE + 16 * wave;
+    src.rows16(src.kh + (uint64_t)(unsigned)row * src.k_rb, src.kofs, to);
+    src.rows16(src.vh + (uint64_t)(unsigned)row * src.v_rb, src.vofs, to + TILE_BYTES);
+  };
+  CacheRows<NB> st;
+  load_queries<NB>(x, c, st.q, lane);
+  fetch(0);
+  fetch(1);
+  fetch(2);
+  c.w = SeqWalk{};
+  begin_part<NB>(x, c, st, lane);
+  CacheLane lo;
+  lo.init(lane);
+  const float c_log2 = x.c_log2;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(st.q.q[nb][ks]));
+  for (int t = 0; t < n; ++t) {
+    MINF_WAIT_VMCNT(16);                       // this wave's part of tile t; those of t + 1 and t + 2 may run
+    __syncthreads();                           // all of tile t is there; all waves are done with tile t - 1
+    fetch(t + 3);                              // behind the last tile it is repeated: every tile issues 8 loads
+    const char *tK = lds + (t & 3) * (2 * TILE_BYTES), *tV = tK + TILE_BYTES;
+    f32x4 s[4][NB];                            // [16 keys][row block]
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const bf16x8 a = lds_read_k(tK, lo.k[ks] + kt * HALF_TILE_ROWS);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+          s[kt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, st.q.q[nb][ks], ks == 0 ? zero : s[kt][nb], 0, 0, 0);
+        }
+      }
+    bool outgrown = false;
+    float mx[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      mx[nb] = s[0][nb][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx[nb] = fmaxf(mx[nb], s[e >> 2][nb][e & 3]);
+      outgrown = outgrown || mx[nb] * c_log2 > st.m[nb] + REF_ROOM;
+    }
+    if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float most = fmaxf(mx[nb], __shfl_xor(mx[nb], 16));
+        most = fmaxf(most, __shfl_xor(most, 32)) * c_log2;
+        const float m_new = fmaxf(st.m[nb], most);
+        const float f = m_new == -INFINITY ? 1.f : fast_exp2(st.m[nb] - m_new);
+        st.m[nb] = m_new;
+        st.l[nb] *= f;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) st.o[nb][db] *= f;
+      }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      bf16x8 p[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const float m = st.m[nb] == -INFINITY ? 0.f : st.m[nb];
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const f32x4 &v4 = s[2 * half + (e >> 2)][nb];
+          const f32x2 v = {fast_exp2(fmaf(v4[e & 3], c_log2, -m)), fast_exp2(fmaf(v4[(e & 3) + 1], c_log2, -m))};
+          sum += v[0] + v[1];
+          const bf16x2 two = __builtin_convertvector(v, bf16x2);
+          p[nb][e] = two[0];
+          p[nb][e + 1] = two[1];
+        }
+        st.l[nb] += sum;
+      }
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        const int at = lo.v[db] + half * HALF_BYTES;
+        const bf16x8 a = lds_read_vt(tV, at, at + HALF_TILE_ROWS);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb], st.o[nb][db], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);        // LDS reads done
+  }
+  MINF_WAIT_VMCNT(0);                          // the repeated loads
+  const int64_t item = ((int64_t)head * x.c_row_tiles + rt) * x.c_splits + part;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int in_tile = (wave * NB + nb) * 16 + (lane & 15);
+    float l = st.l[nb] + __shfl_xor(st.l[nb], 16);
+    l += __shfl_xor(l, 32);
+    if (rt * x.c_tile_rows + in_tile >= x.c_rows) continue;
+    const int64_t at = item * x.c_tile_rows + in_tile;
+    if (lane < 16) x.common_ml[at] = float2{st.m[nb], l};
+    float *to = x.common_o + at * D + 4 * (lane >> 4);
+#pragma unroll
+    for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(to + 16 * db) = st.o[nb][db];
   }
 }
 
@@ -786,8 +919,8 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   };
   auto join = [&](const PieceList &pieces) { add(x.piece_ml, x.piece_o, pieces.count(), [&](int i) { return pieces.at(i); }); };
   auto common = [&](const SeqWalk &c, int head, int crow) {
-    const int64_t at = ((int64_t)head * x.c_row_tiles + crow / 256) * x.c_splits;
-    add(x.common_ml, x.common_o, common_parts(c.s2 / COMMON_TILE, x.c_splits), [&](int i) { return (at + i) * 256 + crow % 256; });
+    const int64_t at = ((int64_t)head * x.c_row_tiles + crow / x.c_tile_rows) * x.c_splits;
+    add(x.common_ml, x.common_o, common_parts(c.s2 / COMMON_TILE, x.c_splits), [&](int i) { return (at + i) * x.c_tile_rows + crow % x.c_tile_rows; });
   };
   if (token) {
     if (x.own_common) common(w, seg, row);
@@ -1230,8 +1363,21 @@ static hipError_t launch_workers(const CacheCall &x, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int NB>
+static hipError_t launch_shared(const CacheCall &x, hipStream_t st) {
+  const size_t lds = 4 * 2 * TILE_BYTES;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_shared_kernel<NB>),
+                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  const int groups = (x.p_common ? 1 : x.batch) * x.n_kv * x.c_splits;
+  hipLaunchKernelGGL(cache_shared_kernel<NB>, dim3((groups + 7) / 8 * 8 * x.c_row_tiles), dim3(64 * CACHE_WAVES), lds, st, x);
+  return hipGetLastError();
+}
+
 hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
-  hipError_t e = x.p_common || x.own_common ? launch_cache_common(x, st) : hipSuccess;
+  hipError_t e = hipSuccess;
+  if (x.p_common || x.own_common)
+    e = x.c_tile_rows == 64 ? launch_shared<1>(x, st) : x.c_tile_rows == 128 ? launch_shared<2>(x, st) : launch_cache_common(x, st);
   if (e != hipSuccess) return e;
   e = x.row_blocks == 1 ? launch_workers<1>(x, st) : launch_workers<2>(x, st);
   if (e != hipSuccess) return e;

@@ -232,17 +232,18 @@ struct CacheCall {
   int32_t rows, row_tiles;              // rows of a K/V head (group * n_new), in tiles of 16 row_blocks
   int32_t p_cap, p_row_tiles;           // capacity of the prefix (0: none), row tiles of its batch * rows rows
   int32_t row_blocks, workers, max_tiles, slot_rows;
-  // The slots that every row sees, in whole tiles of 64, are taken by cache_common_kernel, 256 rows at a time:
-  // of the prefix (p_common) or of every sequence (own_common); the workers take the rest.
-  int32_t p_common, own_common, c_rows, c_row_tiles, c_splits, direct;   // direct: workers may write O themselves
+  // The slots that every row sees, in whole tiles of 64, are taken by cache_shared_kernel (64 or 128 rows at a
+  // time) or cache_common_kernel (256): of the prefix (p_common) or of every sequence (own_common); the workers take
+  // the rest.  direct: workers may write O themselves.
+  int32_t p_common, own_common, c_rows, c_tile_rows, c_row_tiles, c_splits, direct;
   float c_log2;
   // workspace
   float *logits;                        // [sequence, K/V head, max_tiles][rows][32], base 2; NULL: not kept
   float2 *stat;                         // [sequence, K/V head, rows]: reference, sum; NULL: no weights
   float2 *piece_ml;                     // [2 workers + segments][slot_rows]: reference, sum
   float *piece_o;                       // [2 workers + segments][slot_rows][128]
-  float2 *common_ml;                    // [K/V head (of a sequence), c_row_tiles][c_splits][256]
-  float *common_o;                      // [K/V head (of a sequence), c_row_tiles][c_splits][256][128]
+  float2 *common_ml;                    // [K/V head (of a sequence), c_row_tiles][c_splits][c_tile_rows]
+  float *common_o;                      // [K/V head (of a sequence), c_row_tiles][c_splits][c_tile_rows][128]
 };
 hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st);
 hipError_t launch_cache_common(const CacheCall &x, hipStream_t st);     // attn_kernels.hip
