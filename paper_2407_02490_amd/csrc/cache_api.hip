@@ -120,15 +120,17 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   x.c_log2 = scale * 1.4426950408889634f;
   x.rows = x.group * x.n_new;
   const int64_t p_rows = prefix ? (int64_t)x.batch * x.rows : 0;
-  const int64_t most = p_rows > x.rows ? p_rows : x.rows;
-  x.row_blocks = most <= 16 ? 1 : 2;
-  const int tile_rows = 16 * x.row_blocks;
-  x.row_tiles = (x.rows + tile_rows - 1) / tile_rows;
-  x.slot_rows = prefix || x.rows > tile_rows ? tile_rows : x.rows;
   const bool whole_cache = x.n_local == x.capacity;
   x.p_common = prefix && p_rows > 32 && prefix->capacity >= COMMON_TILE;
   x.own_common = !prefix && x.rows > 32 && whole_cache && x.capacity >= 2 * COMMON_TILE;
   x.direct = !prefix && !x.own_common;
+  // The workers' row tiles: one block of 16 rows or two.  Of a prefix whose common slots are another kernel's only a
+  // rest of less than 64 slots is theirs, so that the sequences' own rows decide.
+  const int64_t most = x.p_common || p_rows < x.rows ? x.rows : p_rows;
+  x.row_blocks = most <= 16 ? 1 : 2;
+  const int tile_rows = 16 * x.row_blocks;
+  x.row_tiles = (x.rows + tile_rows - 1) / tile_rows;
+  x.slot_rows = prefix || x.rows > tile_rows ? tile_rows : x.rows;
   // the longest walk: sink and window, each with a tile that it fills in part
   const int64_t visible = (int64_t)x.n_init + x.n_local + x.n_new + 2 * CACHE_TILE;
   x.max_tiles = (int32_t)(((visible < x.capacity ? visible : x.capacity) + CACHE_TILE - 1) / CACHE_TILE);

@@ -93,6 +93,8 @@ WINDOW = [
     (1, 2, 1, 1, 9000, [8999], 0, BIG, "head"),             # more tiles than ... one per worker
     (1, 8, 8, 1, 20000, [20000], 1024, 4096, "head"),
     (5, 8, 2, 2, 3000, [3000, 64, 65, 2999, 31], 40, 1000, "token"),
+    (2, 8, 2, 20, 1000, [1000, 84], 0, BIG, "token"),       # 80 rows that see the whole cache
+    (2, 16, 2, 40, 1500, [1500, 39], 0, BIG, "head"),       # 320 rows
 ]
 
 
@@ -238,6 +240,9 @@ PREFIX = [
     (2, 4, 4, 3, 700, 700, 40, [40, 2]),                     # fewer tokens than rows
     (3, 4, 2, 1, 80, 0, 200, [200, 5, 100]),                 # an empty prefix
     (9, 28, 4, 1, 1000, 999, 70, [70, 1, 69, 33, 32, 31, 2, 9, 64]),
+    (25, 8, 2, 1, 1000, 937, 40, list(range(1, 26))),        # 100 rows
+    (10, 8, 2, 1, 64, 64, 40, list(range(1, 11))),           # 40 rows, one tile
+    (24, 4, 1, 1, 200, 63, 40, list(range(1, 25))),          # 96 rows, less than a tile
     (40, 8, 2, 1, 2100, 2085, 64, list(range(1, 41))),       # 160 rows
     (70, 16, 2, 1, 640, 640, 33, [1 + i % 33 for i in range(70)]),   # 560 rows
     (33, 8, 1, 2, 1300, 1299, 100, [2 + 3 * i for i in range(33)]),  # 528 rows
