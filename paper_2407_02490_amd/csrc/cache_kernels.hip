@@ -883,59 +883,56 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   const bool token = w.i0 + t >= 0;
   const PieceList own = own_pieces(row);
   if (x.direct && w.tiles > 0 && own.p.first == own.p.last) return;    // written by the worker itself
+  // the row's pieces in one list: of the common slots, the workers' of its own segment, of the prefix's
+  const int crow = x.p_common ? b * x.rows + row : row, n_own = w.tiles > 0 ? own.count() : 0;
+  const int64_t common0 = ((int64_t)(x.p_common ? kvh : seg) * x.c_row_tiles + crow / max(x.c_tile_rows, 1)) * x.c_splits;
+  int n_common = 0, n = 0;
+  PieceList pre_pieces = own;
+  if (token) {
+    if (x.own_common) n_common = common_parts(w.s2 / COMMON_TILE, x.c_splits);
+    if (x.p_common) n_common = common_parts(pw.s2 / COMMON_TILE, x.c_splits);
+    n = n_common + n_own;
+    if (x.p_cap > 0 && pw.tiles > 0) {
+      const int prow = b * x.rows + row, prt = prow / tile_rows;
+      pre_pieces.t0 = (kvh * x.p_row_tiles + prt) * pw.places() + SEGMENT_COST;
+      pre_pieces.p = segment_pieces(pre_pieces.t0, pre_pieces.t0 + pw.tiles, share);
+      pre_pieces.segment = kvh * x.p_row_tiles + prt;
+      pre_pieces.base = prow - prt * tile_rows;
+      n += pre_pieces.count();
+    }
+  }
   float m = -INFINITY, l = 0.f;
   f32x2 o = {0.f, 0.f};
-  // every fourth of n pieces, from the wave's first on
-  auto add = [&](const float2 *all_ml, const float *all_o, int n, auto place) {
-    for (int i0 = W == 4 ? wave : 0; i0 < n; i0 += W * JOIN_AHEAD) {
-      float2 ml[JOIN_AHEAD];
-      f32x2 po[JOIN_AHEAD];
+  for (int i0 = W == 4 ? wave : 0; i0 < n; i0 += W * JOIN_AHEAD) {
+    float2 ml[JOIN_AHEAD];
+    f32x2 po[JOIN_AHEAD];
 #pragma unroll
-      for (int j = 0; j < JOIN_AHEAD; ++j) {
-        const int64_t at = place(min(i0 + W * j, n - 1));
-        ml[j] = all_ml[at];
-        po[j] = *reinterpret_cast<const f32x2 *>(all_o + at * D + 2 * lane);
-      }
-      float mx = m;
-#pragma unroll
-      for (int j = 0; j < JOIN_AHEAD; ++j) {
-        if (i0 + W * j >= n) ml[j] = float2{-INFINITY, 0.f};
-        mx = fmaxf(mx, ml[j].x);
-      }
-      const float f = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - mx);
-      m = mx;
-      l *= f;
-      o *= f;
-#pragma unroll
-      for (int j = 0; j < JOIN_AHEAD; ++j) {
-        // a piece without a visible key (reference and sum as at its start) counts for nothing
-        const bool none = ml[j].x == -INFINITY && ml[j].y == 0.f;
-        const float g = none ? 0.f : fast_exp2(ml[j].x - m);
-        l += none ? 0.f : ml[j].y * g;
-        o[0] += none ? 0.f : po[j][0] * g;
-        o[1] += none ? 0.f : po[j][1] * g;
-      }
+    for (int j = 0; j < JOIN_AHEAD; ++j) {
+      const int i = min(i0 + W * j, n - 1);
+      const bool c = i < n_common;
+      const int64_t at = c ? (common0 + i) * x.c_tile_rows + crow % max(x.c_tile_rows, 1)
+                           : i < n_common + n_own ? own.at(i - n_common) : pre_pieces.at(i - n_common - n_own);
+      ml[j] = (c ? x.common_ml : x.piece_ml)[at];
+      po[j] = *reinterpret_cast<const f32x2 *>((c ? x.common_o : x.piece_o) + at * D + 2 * lane);
     }
-  };
-  auto join = [&](const PieceList &pieces) { add(x.piece_ml, x.piece_o, pieces.count(), [&](int i) { return pieces.at(i); }); };
-  auto common = [&](const SeqWalk &c, int head, int crow) {
-    const int64_t at = ((int64_t)head * x.c_row_tiles + crow / x.c_tile_rows) * x.c_splits;
-    add(x.common_ml, x.common_o, common_parts(c.s2 / COMMON_TILE, x.c_splits), [&](int i) { return (at + i) * x.c_tile_rows + crow % x.c_tile_rows; });
-  };
-  if (token) {
-    if (x.own_common) common(w, seg, row);
-    if (w.tiles > 0) join(own);
-    if (x.p_cap > 0) {
-      const int prow = b * x.rows + row, prt = prow / tile_rows;
-      if (x.p_common) common(pw, kvh, prow);
-      if (pw.tiles > 0) {
-        PieceList l = own;
-        l.t0 = (kvh * x.p_row_tiles + prt) * pw.places() + SEGMENT_COST;
-        l.p = segment_pieces(l.t0, l.t0 + pw.tiles, share);
-        l.segment = kvh * x.p_row_tiles + prt;
-        l.base = prow - prt * tile_rows;
-        join(l);
-      }
+    float mx = m;
+#pragma unroll
+    for (int j = 0; j < JOIN_AHEAD; ++j) {
+      if (i0 + W * j >= n) ml[j] = float2{-INFINITY, 0.f};
+      mx = fmaxf(mx, ml[j].x);
+    }
+    const float f = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - mx);
+    m = mx;
+    l *= f;
+    o *= f;
+#pragma unroll
+    for (int j = 0; j < JOIN_AHEAD; ++j) {
+      // a piece without a visible key (reference and sum as at its start) counts for nothing
+      const bool none = ml[j].x == -INFINITY && ml[j].y == 0.f;
+      const float g = none ? 0.f : fast_exp2(ml[j].x - m);
+      l += none ? 0.f : ml[j].y * g;
+      o[0] += none ? 0.f : po[j][0] * g;
+      o[1] += none ? 0.f : po[j][1] * g;
     }
   }
   if (W == 4) {
@@ -1097,23 +1094,48 @@ struct SelectLds {
   int part[SELECT_WAVES], pick[3];
 };
 
-// Histogram of the pass's digit over the slots from .. to - 1 whose higher digits are those of `prefix`.  Lanes
-// add into four copies: weights cluster, and lanes that meet in a bin go one after the other.
+// The keys of the slots from .. to - 1 (at most 32768) in registers, loaded once: a wave takes consecutive ones, so
+// that it can also number them.
+struct SelectKeys {
+  static constexpr int BATCHES = 32768 / SELECT_THREADS / SELECT_AHEAD;
+  unsigned k[BATCHES][SELECT_AHEAD];
+  int w0, w1;                      // this wave's slots, those that are chosen by weight among them: in(i)
+  int first;
+  __device__ inline int slot(int t, int j, int lane) const { return w0 + 64 * (t * SELECT_AHEAD + j) + lane; }
+  __device__ inline bool batch(int t) const { return w0 + 64 * SELECT_AHEAD * t < w1; }
+  __device__ inline bool in(int i) const { return i >= first && i < w1; }
+  __device__ inline void load(const SelectRow &r, int from, int to) {
+    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
+    const int per = (to - from + SELECT_THREADS - 1) / SELECT_THREADS * 64;
+    first = r.first;
+    w0 = from + wave * per;
+    w1 = min(w0 + per, min(to, r.last));
+#pragma unroll
+    for (int t = 0; t < BATCHES; ++t) {
+      if (!batch(t)) break;
+      float v[SELECT_AHEAD];
+#pragma unroll
+      for (int j = 0; j < SELECT_AHEAD; ++j) v[j] = r.w[min(slot(t, j, lane), w1 - 1)];
+#pragma unroll
+      for (int j = 0; j < SELECT_AHEAD; ++j) k[t][j] = weight_key(v[j]);
+    }
+  }
+};
+
+// Histogram of the pass's digit over the keys whose higher digits are those of `prefix`.  Lanes add into four
+// copies: weights cluster, and lanes that meet in a bin go one after the other.
 template <int PASS>
-__device__ inline void select_count(const SelectRow &r, int from, int to, unsigned prefix, SelectLds &s) {
-  const int tid = threadIdx.x;
+__device__ inline void select_count(const SelectKeys &keys, unsigned prefix, SelectLds &s) {
+  const int tid = threadIdx.x, lane = tid & 63;
   for (int i = tid; i < SELECT_COPIES * SELECT_BINS; i += SELECT_THREADS) (&s.hist[0][0])[i] = 0;
   __syncthreads();
-  from = max(from, r.first);
-  to = min(to, r.last);
-  for (int i0 = from; i0 < to; i0 += SELECT_AHEAD * SELECT_THREADS) {
-    float v[SELECT_AHEAD];
 #pragma unroll
-    for (int j = 0; j < SELECT_AHEAD; ++j) v[j] = r.w[min(i0 + j * SELECT_THREADS + tid, to - 1)];
+  for (int t = 0; t < SelectKeys::BATCHES; ++t) {
+    if (!keys.batch(t)) break;
 #pragma unroll
     for (int j = 0; j < SELECT_AHEAD; ++j) {
-      const unsigned k = weight_key(v[j]);
-      if (i0 + j * SELECT_THREADS + tid < to && (k & select_mask(PASS)) == prefix)
+      const unsigned k = keys.k[t][j];
+      if (keys.in(keys.slot(t, j, lane)) && (k & select_mask(PASS)) == prefix)
         atomicAdd(&s.hist[tid & (SELECT_COPIES - 1)][(k >> select_shift(PASS)) & (select_bins(PASS) - 1)], 1);
     }
   }
@@ -1142,37 +1164,21 @@ __device__ inline unsigned select_pick(const int (&n)[2], const int (&n_before)[
   return (unsigned)d;
 }
 
-// Writes the kept slots among from .. to - 1 (a wave takes consecutive ones) behind the `gt` larger and `eq`
-// equal ones of lower slots; of the equal ones the first `want` stay.
-__device__ inline void select_emit(const SelectRow &r, int from, int to, unsigned key, int want, int gt, int eq, int32_t *kept,
-                                   int keep, SelectLds &s) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (to - from + SELECT_THREADS - 1) / SELECT_THREADS * 64;
-  const int w0 = from + wave * per, w1 = min(w0 + per, min(to, r.last));
+// Writes the kept slots among from .. to - 1 behind the `gt` larger and `eq` equal ones of lower slots; of the equal
+// ones the first `want` stay.
+__device__ inline void select_emit(const SelectRow &r, const SelectKeys &keys, int from, int to, unsigned key, int want, int gt,
+                                   int eq, int32_t *kept, int keep, SelectLds &s) {
+  const int tid = threadIdx.x, lane = tid & 63;
   const unsigned long long below = (1ull << lane) - 1;
-  // keys of SELECT_AHEAD * 64 slots from i0 on, with their loads in flight
-  auto look = [&](int i0, unsigned (&k)[SELECT_AHEAD]) {
-    float v[SELECT_AHEAD];
-#pragma unroll
-    for (int j = 0; j < SELECT_AHEAD; ++j) v[j] = r.w[min(i0 + 64 * j + lane, w1 - 1)];
-#pragma unroll
-    for (int j = 0; j < SELECT_AHEAD; ++j) k[j] = weight_key(v[j]);
-  };
-  auto in = [&](int i) { return i >= r.first && i < w1; };
-  // a wave's keys stay in registers between the counting and the writing
-  constexpr int BATCH = 64 * SELECT_AHEAD, BATCHES = 32768 / SELECT_THREADS / SELECT_AHEAD;
-  unsigned k[BATCHES][SELECT_AHEAD];
   int ng = 0, ne = 0;
 #pragma unroll
-  for (int t = 0; t < BATCHES; ++t) {
-    const int i0 = w0 + t * BATCH;
-    if (i0 >= w1) break;
-    look(i0, k[t]);
+  for (int t = 0; t < SelectKeys::BATCHES; ++t) {
+    if (!keys.batch(t)) break;
 #pragma unroll
     for (int j = 0; j < SELECT_AHEAD; ++j) {
-      const bool here = in(i0 + 64 * j + lane);
-      ng += __popcll(__builtin_amdgcn_ballot_w64(here && k[t][j] > key));
-      ne += __popcll(__builtin_amdgcn_ballot_w64(here && k[t][j] == key));
+      const bool here = keys.in(keys.slot(t, j, lane));
+      ng += __popcll(__builtin_amdgcn_ballot_w64(here && keys.k[t][j] > key));
+      ne += __popcll(__builtin_amdgcn_ballot_w64(here && keys.k[t][j] == key));
     }
   }
   int all;
@@ -1180,13 +1186,14 @@ __device__ inline void select_emit(const SelectRow &r, int from, int to, unsigne
   gt += uni(before_g);
   eq += uni(before_e);
 #pragma unroll
-  for (int t = 0; t < BATCHES; ++t) {
-    const int i0 = w0 + t * BATCH;
-    if (i0 >= w1) break;
+  for (int t = 0; t < SelectKeys::BATCHES; ++t) {
+    if (!keys.batch(t)) break;
 #pragma unroll
     for (int j = 0; j < SELECT_AHEAD; ++j) {
-      const int i = i0 + 64 * j + lane;
-      const unsigned long long g = __builtin_amdgcn_ballot_w64(in(i) && k[t][j] > key), e = __builtin_amdgcn_ballot_w64(in(i) && k[t][j] == key);
+      const int i = keys.slot(t, j, lane);
+      const bool here = keys.in(i);
+      const unsigned long long g = __builtin_amdgcn_ballot_w64(here && keys.k[t][j] > key);
+      const unsigned long long e = __builtin_amdgcn_ballot_w64(here && keys.k[t][j] == key);
       const int gr = gt + __popcll(g & below), er = eq + __popcll(e & below);
       if ((g >> lane) & 1 || ((e >> lane) & 1 && er < want)) kept[r.first + gr + min(er, want)] = i;
       gt += __popcll(g);
@@ -1212,11 +1219,13 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_select_kernel(EvictCall 
   if (r.len <= x.keep) return select_all(r.len, kept, x.keep, tid, SELECT_THREADS);
   unsigned key = ~0u;                         // above every weight: nothing to choose
   int want = r.want, gt = 0, eq = 0;
+  SelectKeys keys;
+  keys.load(r, 0, r.len);
   if (want > 0) {
     key = 0;
     auto pass = [&](auto p) {
       constexpr int P = decltype(p)::value;
-      select_count<P>(r, 0, r.len, key, s);
+      select_count<P>(keys, key, s);
       int n[2] = {0, 0};
       const int none[2] = {0, 0}, hi = select_bins(P) - 1 - 2 * tid;
       if (hi > 0)
@@ -1230,7 +1239,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_select_kernel(EvictCall 
     pass(std::integral_constant<int, 1>{});
     pass(std::integral_constant<int, 2>{});
   }
-  select_emit(r, 0, r.len, key, want, 0, 0, kept, x.keep, s);
+  select_emit(r, keys, 0, r.len, key, want, 0, 0, kept, x.keep, s);
 }
 
 // Long rows: a row in chunks, a workgroup each.  Pass p counts its digit per chunk; the workgroups of the next
@@ -1265,6 +1274,8 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_count_kernel(EvictCall x
   if (r.len <= x.keep || r.want == 0) return;
   // digits so far, rank left, larger slots in the chunks before this one
   SelectState *state = x.state + (int64_t)row * x.chunks + chunk;
+  SelectKeys keys;
+  keys.load(r, from, max(to, from));
   unsigned key = 0;
   int want = r.want, gt = 0, eq = 0;
   if (PASS == 2) { key = state->key; want = state->want; gt = state->gt; }
@@ -1272,7 +1283,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_count_kernel(EvictCall x
     select_from_counts<PASS == 0 ? 0 : PASS - 1>(x, row, chunk, key, want, gt, eq, s);
     if (tid == 0) *state = SelectState{key, want, gt};
   }
-  select_count<PASS>(r, from, to, key, s);
+  select_count<PASS>(keys, key, s);
   unsigned *h = x.hist + (((int64_t)PASS * gridDim.y + row) * x.chunks + chunk) * (SELECT_BINS / 2);
   for (int i = tid; i < select_bins(PASS) / 2; i += SELECT_THREADS) {
     int a = 0, b = 0;
@@ -1290,6 +1301,9 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_emit_kernel(EvictCall x)
   if (chunk == 0 && tid == 0) x.counts[row] = min(r.len, x.keep);
   if (r.len <= x.keep) return select_all(r.len, kept, x.keep, chunk * SELECT_THREADS + tid, x.chunks * SELECT_THREADS);
   const int from = chunk * x.chunk_slots, to = min(from + x.chunk_slots, r.len);
+  if (from >= to) return;
+  SelectKeys keys;
+  keys.load(r, from, to);
   unsigned key = ~0u;
   int want = 0, gt = 0, eq = 0;
   if (r.want > 0) {
@@ -1297,57 +1311,70 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_emit_kernel(EvictCall x)
     key = st.key; want = st.want; gt = st.gt;
     select_from_counts<2>(x, row, chunk, key, want, gt, eq, s);
   }
-  if (from < to) select_emit(r, from, to, key, want, gt, eq, kept, x.keep, s);
+  select_emit(r, keys, from, to, key, want, gt, eq, kept, x.keep, s);
 }
 
-// Moves the kept rows to the slots 0, 1, ...  A workgroup owns one slice of 64 bytes of the rows of K or V of
-// one sequence and K/V head (slices 0..3: K, 4..7: V), or its weights (slice 8), and walks them in ascending
-// order, a chunk into registers, then out.  In place that is safe: the kept slots ascend, so the rows of a
-// later chunk lie behind everything that this chunk overwrites.
-constexpr int MOVE_SLICES = 9, MOVE_ROWS = 256;
-__global__ __launch_bounds__(256) void cache_move_kernel(EvictCall x, int in_place) {
+// Moves the kept rows to the slots 0, 1, ...  In place a workgroup owns one slice of 64 bytes of the rows of K or V of
+// one sequence and K/V head (slices 0..3: K, 4..7: V), or its weights (the last slice), and walks them in ascending
+// order, a chunk into registers, then out: the kept slots ascend, so the rows of a later chunk, which are loaded
+// ahead, lie behind everything that this chunk overwrites.  Into another cache whole rows (slices K, V, weights) in
+// any order.
+constexpr int MOVE_ROWS = 4;                                     // a thread, at a time
+template <bool IN_PLACE>
+__global__ __launch_bounds__(256) void cache_move_kernel(EvictCall x) {
+  constexpr int LANES = IN_PLACE ? 4 : 16, SLICES = 16 / LANES, CHUNK = MOVE_ROWS * 256 / LANES;
   const int slice = blockIdx.x, row = blockIdx.y, b = row / x.n_kv, kvh = row - b * x.n_kv, tid = threadIdx.x;
-  const int n = x.counts[row];
+  const int n = x.counts[row], step = CHUNK * gridDim.z;
   const int32_t *kept = x.kept + (int64_t)row * x.keep;
-  const int step = in_place ? MOVE_ROWS : MOVE_ROWS * gridDim.z;
-  if (slice == 8) {
+  if (slice == 2 * SLICES) {
     const float *from = x.weight + b * x.w_sb + kvh * x.w_sh;
     float *to = x.to_weight + b * x.tw_sb + kvh * x.tw_sh;
-    for (int i0 = blockIdx.z * MOVE_ROWS; i0 < n; i0 += step) {
+    for (int i0 = blockIdx.z * 256; i0 < n; i0 += 256 * gridDim.z) {
       const int i = i0 + tid;
       float v = 0.f;
       if (i < n) v = from[kept[i]];
       asm volatile("" : "+v"(v));
-      __syncthreads();
+      if (IN_PLACE) __syncthreads();                             // every weight of the chunk has been read
       if (i < n) to[i] = v;
     }
-    // in place: behind the reads of all kept weights
-    __syncthreads();
-    for (int i = n + (int)blockIdx.z * MOVE_ROWS + tid; i < x.to_capacity; i += MOVE_ROWS * gridDim.z) to[i] = 0.f;
+    if (IN_PLACE) __syncthreads();
+    for (int i = n + (int)blockIdx.z * 256 + tid; i < x.to_capacity; i += 256 * gridDim.z) to[i] = 0.f;
     if (kvh == 0 && blockIdx.z == 0 && tid == 0) x.to_lens[b] = n;
     return;
   }
-  const bool is_v = slice >= 4;
+  const bool is_v = slice >= SLICES;
   const int64_t f_st = is_v ? x.v_st : x.k_st, t_st = is_v ? x.tv_st : x.tk_st;
-  const bf16_t *from = (is_v ? x.v + b * x.v_sb + kvh * x.v_sh : x.k + b * x.k_sb + kvh * x.k_sh) + 32 * (slice & 3) + 8 * (tid & 3);
-  bf16_t *to = (is_v ? x.to_v + b * x.tv_sb + kvh * x.tv_sh : x.to_k + b * x.tk_sb + kvh * x.tk_sh) + 32 * (slice & 3) + 8 * (tid & 3);
-  for (int i0 = blockIdx.z * MOVE_ROWS; i0 < n; i0 += step) {
-    const int end = min(i0 + MOVE_ROWS, n);
-    if (in_place && kept[end - 1] == end - 1) continue;          // nothing evicted in front of these rows
-    uint4 v[4];
+  const int col = 8 * (LANES * (slice % SLICES) + tid % LANES), lane_row = tid / LANES;
+  const bf16_t *from = (is_v ? x.v + b * x.v_sb + kvh * x.v_sh : x.k + b * x.k_sb + kvh * x.k_sh) + col;
+  bf16_t *to = (is_v ? x.to_v + b * x.tv_sb + kvh * x.tv_sh : x.to_k + b * x.tk_sb + kvh * x.tk_sh) + col;
+  auto load = [&](int i0, uint4 (&v)[MOVE_ROWS]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = i0 + 64 * j + (tid >> 2);
-      v[j] = uint4{0u, 0u, 0u, 0u};
-      if (i < end) v[j] = *reinterpret_cast<const uint4 *>(from + kept[i] * f_st);
+    for (int j = 0; j < MOVE_ROWS; ++j) {
+      const int i = i0 + 256 / LANES * j + lane_row;
+      if (i < n) v[j] = *reinterpret_cast<const uint4 *>(from + kept[i] * f_st);
     }
+  };
+  int i0 = blockIdx.z * CHUNK;
+  if (IN_PLACE) {                                                // chunks in front of which nothing was evicted stay
+    for (int same = 256; same == 256 && i0 < n; i0 += same * CHUNK) {
+      const int at = i0 + tid * CHUNK, last = min(at + CHUNK, n) - 1;
+      same = __syncthreads_count(at < n && kept[last] == last);
+    }
+  }
+  uint4 v[MOVE_ROWS], next[MOVE_ROWS];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
-    __syncthreads();                                             // every row of the chunk has been read
+  for (int j = 0; j < MOVE_ROWS; ++j) v[j] = next[j] = uint4{0u, 0u, 0u, 0u};
+  load(i0, v);
+  for (; i0 < n; i0 += step) {
+    load(i0 + step, next);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = i0 + 64 * j + (tid >> 2);
-      if (i < end) *reinterpret_cast<uint4 *>(to + i * t_st) = v[j];
+    for (int j = 0; j < MOVE_ROWS; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
+    if (IN_PLACE) __syncthreads();                               // every row of the chunk has been read
+#pragma unroll
+    for (int j = 0; j < MOVE_ROWS; ++j) {
+      const int i = i0 + 256 / LANES * j + lane_row;
+      if (i < n) *reinterpret_cast<uint4 *>(to + i * t_st) = v[j];
+      v[j] = next[j];
     }
   }
 }
@@ -1407,9 +1434,12 @@ hipError_t launch_cache_evict(const EvictCall &x, bool in_place, hipStream_t st)
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int chunks = (x.keep + MOVE_ROWS - 1) / MOVE_ROWS;
-  hipLaunchKernelGGL(cache_move_kernel, dim3(MOVE_SLICES, rows, in_place ? 1 : (chunks < 1024 ? chunks : 1024)), dim3(256), 0,
-                     st, x, in_place ? 1 : 0);
+  if (in_place) {
+    hipLaunchKernelGGL(cache_move_kernel<true>, dim3(9, rows), dim3(256), 0, st, x);
+  } else {
+    const int chunks = (x.keep + 16 * MOVE_ROWS - 1) / (16 * MOVE_ROWS);
+    hipLaunchKernelGGL(cache_move_kernel<false>, dim3(3, rows, chunks < 1024 ? chunks : 1024), dim3(256), 0, st, x);
+  }
   return hipGetLastError();
 }
 
