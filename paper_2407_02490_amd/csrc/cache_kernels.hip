@@ -1169,7 +1169,9 @@ __device__ inline unsigned select_pick(const int (&n)[2], const int (&n_before)[
 __device__ inline void select_emit(const SelectRow &r, const SelectKeys &keys, int from, int to, unsigned key, int want, int gt,
                                    int eq, int32_t *kept, int keep, SelectLds &s) {
   const int tid = threadIdx.x, lane = tid & 63;
-  const unsigned long long below = (1ull << lane) - 1;
+  auto rank = [](unsigned long long mask, int base) {              // base + set bits of the lower lanes
+    return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, base));
+  };
   int ng = 0, ne = 0;
 #pragma unroll
   for (int t = 0; t < SelectKeys::BATCHES; ++t) {
@@ -1194,8 +1196,9 @@ __device__ inline void select_emit(const SelectRow &r, const SelectKeys &keys, i
       const bool here = keys.in(i);
       const unsigned long long g = __builtin_amdgcn_ballot_w64(here && keys.k[t][j] > key);
       const unsigned long long e = __builtin_amdgcn_ballot_w64(here && keys.k[t][j] == key);
-      const int gr = gt + __popcll(g & below), er = eq + __popcll(e & below);
-      if ((g >> lane) & 1 || ((e >> lane) & 1 && er < want)) kept[r.first + gr + min(er, want)] = i;
+      if ((g | e) == 0) continue;
+      const int gr = rank(g, gt), er = rank(e, eq);
+      if ((here && keys.k[t][j] > key) || (here && keys.k[t][j] == key && er < want)) kept[r.first + gr + min(er, want)] = i;
       gt += __popcll(g);
       eq += __popcll(e);
     }
