@@ -962,16 +962,23 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   if (x.stat && lane == 0) x.stat[(int64_t)seg * x.rows + row] = float2{m, l};
 }
 
-// The same for more than 16 rows, whose logits would be more bytes than the keys: they are computed anew.  A wave
-// takes 64 keys (K as A operands, in registers) and all rows, 16 at a time; per row block 16 MFMAs and 16
-// exponentials a lane.
+// Weights of more than 16 rows, whose logits would be more bytes than the keys: they are computed anew.  A wave takes
+// 64 keys (K as A operands, in registers) and all rows, 16 at a time; per row block 16 MFMAs and 16 exponentials a
+// lane.  The four waves of a workgroup share the rows: each brings one of four blocks into LDS, as operands, while
+// the four before are used.  (Every wave with loads of its own: 256 rows, 4 heads of 40K tokens, 35 us, half of it
+// for the loads.)
 constexpr int COLUMN_KEYS = 256;                                // per workgroup
 __global__ __launch_bounds__(256, 3) void cache_column_kernel(CacheCall x) {
+  __shared__ bf16x8 rows_q[2][4][4][64];                        // [buffer][row block][k step][lane]
+  __shared__ float rows_m[2][64];
   const int kvh = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4, kb = blockIdx.x * COLUMN_KEYS + wave * 64;
   const int len = uni(min(max(x.lens[b], 0), x.capacity)), i0 = len - x.n_new;
-  if (kb >= len) return;
+  if ((int)blockIdx.x * COLUMN_KEYS >= len) return;
   const int64_t head = (int64_t)b * x.n_kv + kvh;
+  // every row sees every key / no row sees a key
+  const bool whole = kb + 63 <= i0 && (kb + 63 < x.n_init || len - 1 - kb < x.n_local);
+  const bool hidden = kb >= len || (kb >= x.n_init && i0 - (kb + 63) >= x.n_local);
   bf16x8 k[4][4];                                               // [16 keys][k step]
 #pragma unroll
   for (int kt = 0; kt < 4; ++kt) {
@@ -979,55 +986,58 @@ __global__ __launch_bounds__(256, 3) void cache_column_kernel(CacheCall x) {
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) k[kt][ks] = *reinterpret_cast<const bf16x8 *>(row + 32 * ks);
   }
-  // every row sees every key / no row sees a key
-  const bool whole = kb + 63 <= i0 && (kb + 63 < x.n_init || len - 1 - kb < x.n_local);
-  const bool hidden = kb >= x.n_init && i0 - (kb + 63) >= x.n_local;
+  bf16x8 q[4];                                                  // this wave's block of the next four
+  float m;
+  auto load = [&](int r0) {
+    const int at = r0 + 16 * wave + n, row = min(at, x.rows - 1), t = row / x.group;
+    const bf16_t *from = x.q + b * x.q_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.q_sh + t * x.q_st + 8 * g;
+    const float2 ml = x.stat[head * x.rows + row];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) q[ks] = *reinterpret_cast<const bf16x8 *>(from + 32 * ks);
+    // p = 2^(c s - m) / l = 2^(c s - (m + log2 l)); a row without a key, or behind the last: 2^-inf
+    m = at >= x.rows || (ml.x == -INFINITY && ml.y == 0.f) ? INFINITY : ml.x + __builtin_amdgcn_logf(ml.y);
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) rows_q[buf][wave][ks][lane] = q[ks];
+    if (g == 0) rows_m[buf][16 * wave + n] = m;
+  };
   float sum[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-  struct Block {                                                // this lane's row of 16
-    bf16x8 q[4];
-    float2 ml;
-    int t;
-  };
-  auto load = [&](int r0, Block &w) {
-    const int row = min(r0 + n, x.rows - 1);
-    w.t = row / x.group;
-    const bf16_t *q = x.q + b * x.q_sb + (int64_t)(kvh * x.group + row - w.t * x.group) * x.q_sh + w.t * x.q_st + 8 * g;
-    w.ml = x.stat[head * x.rows + row];
+  load(0);
+  store(0);
+  __syncthreads();
+  for (int r0 = 0, buf = 0; r0 < x.rows; r0 += 64, buf ^= 1) {
+    const bool more = r0 + 64 < x.rows;
+    if (more) load(r0 + 64);
+    for (int blk = 0; blk < 4 && r0 + 16 * blk < x.rows && !hidden; ++blk) {
+      const float ref = rows_m[buf][16 * blk + n];
+      f32x4 s[4];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) w.q[ks] = *reinterpret_cast<const bf16x8 *>(q + 32 * ks);
-  };
-  Block ahead;
-  load(0, ahead);
-  for (int r0 = 0; r0 < x.rows && !hidden; r0 += 16) {
-    const Block w = ahead;
-    if (r0 + 16 < x.rows) load(r0 + 16, ahead);
-    const int t = w.t;
-    // p = 2^(c s - m) / l = 2^(c s - (m + log2 l)); a row without a key, or behind the last: 2^-inf
-    const bool none = r0 + n >= x.rows || (w.ml.x == -INFINITY && w.ml.y == 0.f);
-    const float m = none ? INFINITY : w.ml.x + __builtin_amdgcn_logf(w.ml.y);
-    f32x4 s[4];
+      for (int ks = 0; ks < 4; ++ks) {
+        const bf16x8 qf = rows_q[buf][blk][ks][lane];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][ks], w.q[ks], ks == 0 ? zero : s[kt], 0, 0, 0);
+        for (int kt = 0; kt < 4; ++kt) {
+          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+          s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][ks], qf, ks == 0 ? zero : s[kt], 0, 0, 0);
+        }
       }
-    if (whole) {
+      if (whole) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i] += fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -m));
-      continue;
+        for (int i = 0; i < 16; ++i) sum[i] += fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -ref));
+        continue;
+      }
+      const int t = min(r0 + 16 * blk + n, x.rows - 1) / x.group;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const bool sees = cache_visible(kb + 16 * (i >> 2) + 4 * g + (i & 3), i0 + t, x.n_init, x.n_local);
+        const float p = fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -ref));
+        sum[i] += sees ? p : 0.f;
+      }
     }
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool sees = cache_visible(kb + 16 * kt + 4 * g + i, i0 + t, x.n_init, x.n_local);
-        const float p = fast_exp2(fmaf(s[kt][i], x.c_log2, -m));
-        sum[4 * kt + i] += sees ? p : 0.f;
-      }
+    if (more) store(buf ^ 1);                                   // last read a barrier ago
+    __syncthreads();
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i)
