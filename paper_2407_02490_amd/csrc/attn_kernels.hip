@@ -2962,8 +2962,6 @@ __global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
   d.kw = reinterpret_cast<const char *>(c.kh) + (size_t)(16 * wave) * d.k_rb;
   d.vw = reinterpret_cast<const char *>(c.vh) + (size_t)(16 * wave) * d.v_rb;
   d.lds_w = wave * 4096;
-  ashape_first_loads<1>(c, d);
-
   WaveState st;
   auto load_rows = [&]() {
 #pragma unroll
@@ -2993,6 +2991,7 @@ __global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
   mp.q0 = 1 << 30; mp.lo = 0; mp.hi = 1 << 30; mp.n_init = 0; mp.n_local = (1 << 30) + BQ;
   QAcc qa;
   pin_q(qa, st);
+  ashape_first_loads<1>(c, d);             // behind Q: the tiles come from memory, and the first is waited for alone
   bool has_ref = false;
   ashape_pass_pipelined<AllCls, 1>(c, d, st, qa, has_ref, lo, mp, AllCls(), lane);
   if (__syncthreads_or(needs_exact(st) ? 1 : 0)) {
