@@ -766,11 +766,7 @@ struct AllCls {
 //    infinite reference.  The body is one straight path, which keeps the 128
 //    output accumulators in place; the first iteration has no output update,
 //    the last two form logits nobody consumes.
-//  - AHEAD = 1 issues the loads of an iteration one tile further ahead, K(t+4) and V(t+2), into the slots that are
-//    free behind the barrier, and waits for those of two iterations ago: the cache calls, whose tiles come from
-//    memory rather than from the caches, one pass over them (half an iteration is too short for that: 8 K/V
-//    heads of 128K tokens, 128 rows, 124 us at AHEAD = 0).
-template <class Cls, int AHEAD = 0>
+template <class Cls>
 struct AshapeLoop {
   WaveState &st;
   const QAcc &qa;
@@ -790,7 +786,6 @@ struct AshapeLoop {
   static constexpr unsigned k_slot(int i) { return (unsigned)(i & 3) * TILE_BYTES; }
   static constexpr unsigned v_slot(int i) { return (unsigned)(4 + (i & 3)) * TILE_BYTES; }
   int kb1, kb2, kb3, ti3;    // key bases of tiles t+1, t+2, t+3 (indices clamped to T-1); index of the last
-  int kb4 = 0;               // AHEAD: of tile t+4 (ti3: its index)
   int cls_cur;
   bool &has_ref;
 
@@ -802,8 +797,8 @@ struct AshapeLoop {
 
   // for iteration t, from the tile state of iteration t
   __device__ inline void prepare(int t) {
-    kt_ = d.kw + (size_t)(AHEAD ? kb4 : kb3) * d.k_rb;                  // K(t+3) -> slot (t+3) mod 4
-    vt_ = d.vw + (size_t)(AHEAD ? kb2 : kb1) * d.v_rb;                  // V(t+1) -> slot (t+1) mod 4
+    kt_ = d.kw + (size_t)kb3 * d.k_rb;                                  // K(t+3) -> slot (t+3) mod 4
+    vt_ = d.vw + (size_t)kb1 * d.v_rb;                                  // V(t+1) -> slot (t+1) mod 4
     cls_nxt_ = t + 1 < T ? cls.of(kb1) : 0;
   }
 
@@ -842,18 +837,16 @@ struct AshapeLoop {
     }
     // the iteration's scalar operands were prepared during the previous one
     const char *kt = kt_, *vt = vt_;
-    const unsigned k_dst = lds_addr_of(lds) + k_slot(PH + 3 + AHEAD) + d.lds_w;
-    const unsigned v_dst = lds_addr_of(lds) + v_slot(PH + 1 + AHEAD) + d.lds_w;
+    const unsigned k_dst = lds_addr_of(lds) + k_slot(PH + 3) + d.lds_w;
+    const unsigned v_dst = lds_addr_of(lds) + v_slot(PH + 1) + d.lds_w;
     const int cls_nxt = cls_nxt_, kb_nxt = kb1;
     const bool attend_cur = cls_cur != 0;
     // ... and the next one's are prepared in round 5, between MFMAs
     auto prepare_next = [&]() {
       kb1 = kb2; kb2 = kb3;
-      if (AHEAD) kb3 = kb4;
-      int &last = AHEAD ? kb4 : kb3;
       if (ti3 + 1 < T) {
         ++ti3;
-        last = ti3 == T1 ? s2 : last + BK;
+        kb3 = ti3 == T1 ? s2 : kb3 + BK;
       }
       prepare(t + 1);
     };
@@ -941,9 +934,8 @@ struct AshapeLoop {
         // The iteration's one barrier sits in its middle.  Landed and visible behind it: the loads
         // issued in rounds 4..7 of the iteration before, K(t+2) and V(t), which the next iteration
         // reads.  Free behind it: the slots this iteration's loads (rounds 4..7) overwrite, which
-        // held K(t-1) and V(t-3), last read two and three iterations ago.  (AHEAD: landed the loads of the
-        // iteration before that; free K(t) and V(t-2), last read in the iteration before.)
-        if (AHEAD) MINF_WAIT_VMCNT(8); else MINF_WAIT_VMCNT(0);
+        // held K(t-1) and V(t-3), last read two and three iterations ago.
+        MINF_WAIT_VMCNT(0);
         __syncthreads();
       }
     };
@@ -975,7 +967,6 @@ struct AshapeLoop {
 // iteration has no output update.  (Loads behind Q and a zero update: windows of (0, 64) 333 us instead of
 // 323, (128, 1024) 714 instead of 705, 8 heads of 128K tokens; longer ones the same.)  In vs_share_kernel Q
 // is there and a pass does start on K(0) alone.
-template <int AHEAD = 0>
 __device__ inline void ashape_first_loads(const AshapeCtx &c, const WaveDma &d) {
   const unsigned dst = lds_addr_of(c.lds) + d.lds_w;
   auto tile = [&](const char *w, unsigned rb, const DmaRows &rows, int t, unsigned to) {
@@ -987,26 +978,21 @@ __device__ inline void ashape_first_loads(const AshapeCtx &c, const WaveDma &d) 
   tile(d.kw, d.k_rb, d.k, 1, dst + TILE_BYTES);
   tile(d.vw, d.v_rb, d.v, 0, dst + 4 * TILE_BYTES);
   tile(d.kw, d.k_rb, d.k, 2, dst + 2 * TILE_BYTES);
-  if (AHEAD) {
-    tile(d.kw, d.k_rb, d.k, 3, dst + 3 * TILE_BYTES);
-    tile(d.vw, d.v_rb, d.v, 1, dst + 5 * TILE_BYTES);
-  }
 }
 
 // After ashape_first_loads.
-template <class Cls, int AHEAD = 0>
+template <class Cls>
 __device__ inline void ashape_pass_pipelined(const AshapeCtx &c, const WaveDma &d, WaveState &st, const QAcc &qa,
                                              bool &has_ref, const LaneOfs &lo, const MaskP &mp, const Cls &cls,
                                              int lane) {
-  AshapeLoop<Cls, AHEAD> lp{st, qa, lo, mp, d, cls, c.c_log2, lane, c.T, c.T1, c.s2, c.lds, 0, 0, 0, 0, 0, 0, has_ref};
+  AshapeLoop<Cls> lp{st, qa, lo, mp, d, cls, c.c_log2, lane, c.T, c.T1, c.s2, c.lds, 0, 0, 0, 0, 0, has_ref};
   const int last = c.T - 1;
   const int kb0 = lp.tile_base(0);
   lp.kb1 = lp.tile_base(min(1, last)); lp.kb2 = lp.tile_base(min(2, last));
   lp.ti3 = min(3, last); lp.kb3 = lp.tile_base(lp.ti3);
-  if (AHEAD) { lp.ti3 = min(4, last); lp.kb4 = lp.tile_base(lp.ti3); }
   f32x16 sa[2][2], sb[2][2];
   bf16x8 pa[2][2][2], pb[2][2][2];
-  if (AHEAD) MINF_WAIT_VMCNT(20); else MINF_WAIT_VMCNT(12);      // K(0)
+  MINF_WAIT_VMCNT(12);      // K(0)
   __syncthreads();
   lp.cls_cur = lp.cls.of(kb0);
   // also for a tile this wave does not attend: its (finite) logits are turned into P = 0
@@ -1016,10 +1002,10 @@ __device__ inline void ashape_pass_pipelined(const AshapeCtx &c, const WaveDma &
     if (!has_ref) take_reference<2>(sa, st, c.c_log2);
     has_ref = true;
   }
-  if (AHEAD) MINF_WAIT_VMCNT(12); else MINF_WAIT_VMCNT(4);       // K(1), V(0); K(2) is awaited at the barrier of iteration 0
+  MINF_WAIT_VMCNT(4);       // K(1), V(0); K(2) is awaited at the barrier of iteration 0
   __syncthreads();          // all waves are done with K(0)
   lp.prepare(0);
-  typename AshapeLoop<Cls, AHEAD>::Lead lead;
+  typename AshapeLoop<Cls>::Lead lead;
   lp.template read_lead<0, true>(lead);
   // iterations t = 0 .. T (the last one finishes the output update of tile T-1; an update alone behind
   // the loop makes the compiler spill); T is the same for the four waves, which meet at the barrier of
@@ -2928,33 +2914,45 @@ __global__ __launch_bounds__(256) void vs_ring_kernel(QKV x, HeadList hl, const 
 }
 
 // ---------------------------------------------------------------------------
-// Cache calls with many rows per K/V head (a prefix shared by a batch, many new tokens): the slots that every row
-// sees, in whole 64-key tiles.  256 rows share the tiles as in ashape_kernel, without a mask; a workgroup takes
-// one part of the slots of one row tile and leaves its references, sums and unnormalised O in the workspace for
-// cache_join_kernel.  From 33 rows on: the workers of cache_kernels.hip read the slots once per 32 rows, this
-// kernel once per 256, at 1.3 PFLOP/s with all of them in use.
+// A prefix that a batch shares, with more than 128 rows per K/V head: its whole 64-key tiles, which every row sees.
+// 256 rows share the tiles as in ashape_kernel, without a mask; a workgroup takes one part of the tiles of one row
+// tile and leaves its references, sums and unnormalised O in the workspace for cache_join_kernel.  (cache_shared_kernel
+// reads its operands from LDS for 32 rows at a time, this loop for 64: 640 rows, 8 heads of 20K tokens, 99 us there
+// with 256 rows a workgroup, 64 here.)
 // Launch order: the row tiles that read the same slots run on one XCD, one after the other.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
+__global__ __launch_bounds__(256) void cache_prefix_kernel(CacheCall x) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int per_xcd = blockIdx.x >> 3, rt = per_xcd % x.c_row_tiles;
-  const int group = (per_xcd / x.c_row_tiles) * 8 + (blockIdx.x & 7);        // (K/V head of a sequence, part of the slots)
-  const int heads = (x.p_common ? 1 : x.batch) * x.n_kv;
-  if (group >= heads * x.c_splits) return;
-  const int head = group / x.c_splits, part = group - head * x.c_splits;
-  const int b = x.p_common ? 0 : head / x.n_kv, kvh = head - b * x.n_kv;
-  const int len = x.p_common ? x.p_lens[0] : x.lens[b], cap = x.p_common ? x.p_cap : x.capacity;
-  const int tiles = to_sgpr(common_slots((len < 0 ? 0 : min(len, cap)) - (x.p_common ? 1 : x.n_new)) / COMMON_TILE);
-  const int per = common_share(tiles, x.c_splits), t0 = to_sgpr(part * per), n = to_sgpr(min(per, tiles - t0));
+  const SharedPart &sh = x.p_sh;
+  const int per_xcd = blockIdx.x >> 3, rt = per_xcd % sh.row_tiles;
+  const int group = (per_xcd / sh.row_tiles) * 8 + (blockIdx.x & 7);         // (K/V head, part of the tiles)
+  if (group >= x.n_kv * sh.splits) return;
+  const int kvh = group / sh.splits, part = group - kvh * sh.splits;
+  const int tiles = to_sgpr(min(max(x.p_lens[0], 0), x.p_cap) / SHARED_TILE);
+  const int per = part_tiles(tiles, sh.splits), t0 = to_sgpr(part * per), n = to_sgpr(min(per, tiles - t0));
   if (n <= 0) return;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  WaveState st;
+  auto load_rows = [&]() {
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb) {
+      const int at = min(rt * 256 + wave * 64 + 32 * nb + (lane & 31), sh.rows - 1);   // rows behind the last repeat it
+      const int b = at / x.rows, row = at - b * x.rows, t = row / x.group;
+      const bf16_t *q = x.q + b * x.q_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.q_sh + t * x.q_st + 8 * (lane >> 5);
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) st.q[nb][ks] = *reinterpret_cast<const bf16x8 *>(q + 16 * ks);
+    }
+  };
+  load_rows();
+  QAcc qa;
+  pin_q(qa, st);                           // awaited ahead of the tiles: those come from memory, and the first is waited for alone
   AshapeCtx c;
-  c.k_st = x.p_common ? x.pk_st : x.k_st; c.v_st = x.p_common ? x.pv_st : x.v_st;
-  c.kh = (x.p_common ? x.pk + kvh * x.pk_sh : x.k + b * x.k_sb + kvh * x.k_sh) + (int64_t)t0 * COMMON_TILE * c.k_st;
-  c.vh = (x.p_common ? x.pv + kvh * x.pv_sh : x.v + b * x.v_sb + kvh * x.v_sh) + (int64_t)t0 * COMMON_TILE * c.v_st;
-  c.N = n * COMMON_TILE; c.T1 = 0; c.T = n; c.s2 = 0; c.lds = lds; c.c_log2 = x.c_log2;
+  c.k_st = x.pk_st; c.v_st = x.pv_st;
+  c.kh = x.pk + kvh * x.pk_sh + (int64_t)t0 * SHARED_TILE * c.k_st;
+  c.vh = x.pv + kvh * x.pv_sh + (int64_t)t0 * SHARED_TILE * c.v_st;
+  c.N = n * SHARED_TILE; c.T1 = 0; c.T = n; c.s2 = 0; c.lds = lds; c.c_log2 = x.c_log2;
   WaveDma d;
   d.k_rb = (unsigned)c.k_st * 2u; d.v_rb = (unsigned)c.v_st * 2u;
   d.k.init(d.k_rb, lane);
@@ -2962,20 +2960,7 @@ __global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
   d.kw = reinterpret_cast<const char *>(c.kh) + (size_t)(16 * wave) * d.k_rb;
   d.vw = reinterpret_cast<const char *>(c.vh) + (size_t)(16 * wave) * d.v_rb;
   d.lds_w = wave * 4096;
-  WaveState st;
-  auto load_rows = [&]() {
-#pragma unroll
-    for (int nb = 0; nb < 2; ++nb) {
-      int row = min(rt * 256 + wave * 64 + 32 * nb + (lane & 31), x.c_rows - 1);   // rows behind the last repeat it
-      int rb = b;
-      if (x.p_common) { rb = row / x.rows; row -= rb * x.rows; }
-      const int t = row / x.group;
-      const bf16_t *q = x.q + rb * x.q_sb + (int64_t)(kvh * x.group + row - t * x.group) * x.q_sh + t * x.q_st + 8 * (lane >> 5);
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) st.q[nb][ks] = *reinterpret_cast<const bf16x8 *>(q + 16 * ks);
-    }
-  };
-  load_rows();
+  ashape_first_loads(c, d);
 #pragma unroll
   for (int nb = 0; nb < 2; ++nb) {
     set_reference(st, nb, 0.f);
@@ -2989,11 +2974,8 @@ __global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
   lane_offsets(lo, lane);
   MaskP mp;                                // every key of the part, for the rows of all waves
   mp.q0 = 1 << 30; mp.lo = 0; mp.hi = 1 << 30; mp.n_init = 0; mp.n_local = (1 << 30) + BQ;
-  QAcc qa;
-  pin_q(qa, st);
-  ashape_first_loads<1>(c, d);             // behind Q: the tiles come from memory, and the first is waited for alone
   bool has_ref = false;
-  ashape_pass_pipelined<AllCls, 1>(c, d, st, qa, has_ref, lo, mp, AllCls(), lane);
+  ashape_pass_pipelined<AllCls>(c, d, st, qa, has_ref, lo, mp, AllCls(), lane);
   if (__syncthreads_or(needs_exact(st) ? 1 : 0)) {
     load_rows();
     reset_for_max_pass(st);
@@ -3001,15 +2983,15 @@ __global__ __launch_bounds__(256) void cache_common_kernel(CacheCall x) {
     finish_max_pass(st, x.c_log2);
     ashape_pass<PASS_FIX>(c, st, lo, mp, wave, lane);
   }
-  const int64_t item = ((int64_t)head * x.c_row_tiles + rt) * x.c_splits + part;
+  const int64_t item = ((int64_t)kvh * sh.row_tiles + rt) * sh.splits + part;
 #pragma unroll
   for (int nb = 0; nb < 2; ++nb) {
     const int in_tile = wave * 64 + 32 * nb + (lane & 31), h = lane >> 5;
     const float l = st.l[nb] + __shfl_xor(st.l[nb], 32);
-    if (rt * 256 + in_tile >= x.c_rows) continue;
+    if (rt * 256 + in_tile >= sh.rows) continue;
     const int64_t at = item * 256 + in_tile;
-    if (h == 0) x.common_ml[at] = float2{st.m[nb], l};
-    float *to = x.common_o + at * D + 4 * h;
+    if (h == 0) sh.ml[at] = float2{st.m[nb], l};
+    float *to = sh.o + at * D + 4 * h;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -3026,12 +3008,11 @@ static hipError_t set_lds(const void *fn, size_t bytes) {
   return hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-hipError_t launch_cache_common(const CacheCall &x, hipStream_t st) {
+hipError_t launch_cache_prefix(const CacheCall &x, hipStream_t st) {
   const size_t lds = 8 * TILE_BYTES;
-  hipError_t e = set_lds(reinterpret_cast<const void *>(cache_common_kernel), lds);
+  hipError_t e = set_lds(reinterpret_cast<const void *>(cache_prefix_kernel), lds);
   if (e != hipSuccess) return e;
-  const int groups = (x.p_common ? 1 : x.batch) * x.n_kv * x.c_splits;
-  hipLaunchKernelGGL(cache_common_kernel, dim3((groups + 7) / 8 * 8 * x.c_row_tiles), dim3(256), lds, st, x);
+  hipLaunchKernelGGL(cache_prefix_kernel, dim3((x.n_kv * x.p_sh.splits + 7) / 8 * 8 * x.p_sh.row_tiles), dim3(256), lds, st, x);
   return hipGetLastError();
 }
 

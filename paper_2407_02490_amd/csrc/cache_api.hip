@@ -77,19 +77,22 @@ minf_status check_queries(const minf_queries *x, const minf_kv_cache *c, bool ne
 // Everything but the workspace's addresses; need: its bytes.
 struct Plan {
   CacheCall x;
-  size_t need, at_ml, at_common, at_common_ml, at_stat, at_logits;
+  size_t need, at_ml, at_shared[2], at_shared_ml[2], at_stat, at_logits;     // [0] own, [1] prefix
 };
 
-// Parts that the common slots of `items` row tiles are cut into: as many workgroups, one per CU, in rounds.  A
-// workgroup's start and end cost about as much as six tiles.
-int common_splits(int64_t items, int64_t tiles) {
-  int best = 1;
+// How the rows of `heads` K/V heads (of a sequence) are taken, whole: 256 at a time: row tiles, and parts such that the
+// workgroups, one per CU, come in rounds of least time.  A workgroup's start and end cost as much as six tiles.
+void plan_shared(SharedPart &p, int64_t heads, int64_t rows, int64_t tiles, bool whole) {
+  p.on = 1;
+  p.rows = (int32_t)rows;
+  p.tile_rows = rows <= 64 ? 64 : rows <= 128 || !whole ? 128 : 256;
+  p.row_tiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
+  p.splits = 1;
   int64_t least = INT64_MAX;
   for (int s = 1; s <= 64 && s <= tiles; ++s) {
-    const int64_t time = (items * s + CUS - 1) / CUS * (common_share((int32_t)tiles, s) + 6);
-    if (time < least) { least = time; best = s; }
+    const int64_t time = (heads * p.row_tiles * s + CUS - 1) / CUS * (part_tiles((int32_t)tiles, s) + 6);
+    if (time < least) { least = time; p.splits = s; }
   }
-  return best;
 }
 
 minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_kv_cache *prefix, int32_t n_init,
@@ -120,51 +123,50 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   x.c_log2 = scale * 1.4426950408889634f;
   x.rows = x.group * x.n_new;
   const int64_t p_rows = prefix ? (int64_t)x.batch * x.rows : 0;
-  const bool whole_cache = x.n_local == x.capacity;
-  x.p_common = prefix && p_rows > 32 && prefix->capacity >= COMMON_TILE;
-  x.own_common = !prefix && x.rows > 32 && whole_cache && x.capacity >= 2 * COMMON_TILE;
-  x.direct = !prefix && !x.own_common;
-  // The workers' row tiles: one block of 16 rows or two.  Of a prefix whose common slots are another kernel's only a
-  // rest of less than 64 slots is theirs, so that the sequences' own rows decide.
-  const int64_t most = x.p_common || p_rows < x.rows ? x.rows : p_rows;
+  // rows that the workers take: up to 32, in one block of 16 or two
+  const bool own_sh = x.rows > 32, p_sh = p_rows > 32;
+  // (of a prefix of more than 128 rows only a rest of less than 64 slots)
+  const int64_t most = own_sh ? (p_sh ? 0 : p_rows) : p_sh || p_rows < x.rows ? x.rows : p_rows;
   x.row_blocks = most <= 16 ? 1 : 2;
   const int tile_rows = 16 * x.row_blocks;
-  x.row_tiles = (x.rows + tile_rows - 1) / tile_rows;
+  x.row_tiles = own_sh ? 0 : (x.rows + tile_rows - 1) / tile_rows;
+  x.p_row_tiles = p_sh && p_rows <= 128 ? 0 : (int32_t)((p_rows + tile_rows - 1) / tile_rows);
   x.slot_rows = prefix || x.rows > tile_rows ? tile_rows : x.rows;
+  x.direct = !prefix;
   // the longest walk: sink and window, each with a tile that it fills in part
-  const int64_t visible = (int64_t)x.n_init + x.n_local + x.n_new + 2 * CACHE_TILE;
-  x.max_tiles = (int32_t)(((visible < x.capacity ? visible : x.capacity) + CACHE_TILE - 1) / CACHE_TILE);
+  const int64_t visible = (int64_t)x.n_init + x.n_local + x.n_new + 2 * SHARED_TILE, seen = visible < x.capacity ? visible : x.capacity;
+  x.max_tiles = (int32_t)((seen + CACHE_TILE - 1) / CACHE_TILE);
   int64_t segments = (int64_t)x.batch * x.n_kv * x.row_tiles;
   int64_t places = segments * (x.max_tiles + SEGMENT_COST);
+  if (own_sh) plan_shared(x.own_sh, (int64_t)x.batch * x.n_kv, x.rows, (seen + SHARED_TILE - 1) / SHARED_TILE, false);
   if (prefix) {
     x.pk = static_cast<const bf16_t *>(prefix->k); x.pv = static_cast<const bf16_t *>(prefix->v);
     x.p_lens = prefix->lens;
     x.pk_sh = prefix->k_stride[1]; x.pk_st = prefix->k_stride[2];
     x.pv_sh = prefix->v_stride[1]; x.pv_st = prefix->v_stride[2];
     x.p_cap = prefix->capacity;
-    x.p_row_tiles = (int32_t)((p_rows + tile_rows - 1) / tile_rows);
     segments += (int64_t)x.n_kv * x.p_row_tiles;
     places += (int64_t)x.n_kv * x.p_row_tiles * ((prefix->capacity + CACHE_TILE - 1) / CACHE_TILE + SEGMENT_COST);
+    if (p_sh) plan_shared(x.p_sh, x.n_kv, p_rows, (prefix->capacity + SHARED_TILE - 1) / SHARED_TILE, true);
   }
   if (places >= (int64_t)1 << 30) return MINF_ERR_SHAPE;               // the list of tiles is counted in 32 bits
   x.workers = CUS * 4;
-  // workspace: O of the pieces, their maxima and sums, the same of the common slots' parts, statistics of the
-  // rows, logits (for the weights of up to 16 rows)
-  const size_t slots = ((size_t)2 * x.workers + (size_t)segments) * x.slot_rows;
+  // workspace: O of the pieces, their references and sums, the same of the rows that waves take together, statistics
+  // of the rows, logits (for the weights of up to 16 rows)
+  const size_t slots = segments > 0 ? ((size_t)2 * x.workers + (size_t)segments) * x.slot_rows : 0;
   const size_t heads = (size_t)x.batch * x.n_kv;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   p.at_ml = up(slots * 128 * sizeof(float));
-  p.at_common = p.at_common_ml = p.at_stat = p.at_ml + up(slots * sizeof(float2));
-  if (x.p_common || x.own_common) {
-    x.c_rows = (int32_t)(prefix ? p_rows : x.rows);
-    x.c_tile_rows = x.c_rows <= 64 ? 64 : x.c_rows <= 128 ? 128 : 256;
-    x.c_row_tiles = (x.c_rows + x.c_tile_rows - 1) / x.c_tile_rows;
-    const int64_t items = (int64_t)(prefix ? 1 : x.batch) * x.n_kv * x.c_row_tiles;
-    x.c_splits = common_splits(items, (prefix ? prefix->capacity : x.capacity) / COMMON_TILE);
-    if ((items + 8) * x.c_splits > MAX_BLOCKS) return MINF_ERR_SHAPE;
-    const size_t rows = (size_t)items * x.c_splits * x.c_tile_rows;
-    p.at_common_ml = p.at_common + up(rows * 128 * sizeof(float));
-    p.at_stat = p.at_common_ml + up(rows * sizeof(float2));
+  p.at_stat = p.at_ml + up(slots * sizeof(float2));
+  for (int i = 0; i < 2; ++i) {
+    const SharedPart &sh = i ? x.p_sh : x.own_sh;
+    p.at_shared[i] = p.at_shared_ml[i] = p.at_stat;
+    if (!sh.on) continue;
+    const int64_t items = (int64_t)(i ? x.n_kv : heads) * sh.row_tiles * sh.splits;
+    if (items + 8 * sh.row_tiles > MAX_BLOCKS / 2) return MINF_ERR_SHAPE;
+    if (!i && sh.splits == 1 && x.direct) continue;                    // O is final
+    p.at_shared_ml[i] = p.at_shared[i] + up((size_t)items * sh.tile_rows * 128 * sizeof(float));
+    p.at_stat = p.at_shared_ml[i] + up((size_t)items * sh.tile_rows * sizeof(float2));
   }
   p.at_logits = p.need = p.at_stat;
   if (weights != MINF_WEIGHTS_NONE) {
@@ -207,8 +209,11 @@ minf_status run_plan(const minf_queries *q, const minf_kv_cache *c, const minf_k
   char *w = static_cast<char *>(ws);
   p.x.piece_o = reinterpret_cast<float *>(w);
   p.x.piece_ml = reinterpret_cast<float2 *>(w + p.at_ml);
-  p.x.common_o = reinterpret_cast<float *>(w + p.at_common);
-  p.x.common_ml = reinterpret_cast<float2 *>(w + p.at_common_ml);
+  for (int i = 0; i < 2; ++i) {
+    SharedPart &sh = i ? p.x.p_sh : p.x.own_sh;
+    sh.o = reinterpret_cast<float *>(w + p.at_shared[i]);
+    sh.ml = reinterpret_cast<float2 *>(w + p.at_shared_ml[i]);
+  }
   if (weights != MINF_WEIGHTS_NONE) {
     p.x.stat = reinterpret_cast<float2 *>(w + p.at_stat);
     if (p.x.rows <= 16) p.x.logits = reinterpret_cast<float *>(w + p.at_logits);

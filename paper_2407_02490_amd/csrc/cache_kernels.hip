@@ -46,7 +46,7 @@ struct CachePart {
 // Lengths: `mine` holds those of the first 64 sequences, one a lane, loaded once.
 template <class X>
 __device__ inline SeqWalk walk_of_len(X &x, int len) {
-  return seq_walk(len, x.capacity, x.n_new, x.n_init, x.n_local, x.own_common);
+  return seq_walk(len, x.capacity, x.n_new, x.n_init, x.n_local);
 }
 template <class X>
 __device__ inline int first_lens(X &x, int lane) { return lane < x.batch ? x.lens[lane] : 0; }
@@ -58,10 +58,12 @@ template <class X>
 __device__ inline SeqWalk walk_of(X &x, int b, int mine) {     // wave-uniform
   return walk_of_len(x, b < 64 ? __builtin_amdgcn_readlane(mine, b) : uni(x.lens[uni(b)]));
 }
-// The prefix: every row sees all of it.
+// What the workers take of the prefix, which every row sees: all of it, or what cache_prefix_kernel leaves.  (Nothing
+// where there are no row tiles of theirs.)
 template <class X>
 __device__ inline SeqWalk prefix_walk(X &x) {
-  return seq_walk(x.p_cap > 0 ? uni(x.p_lens[0]) : 0, x.p_cap, 1, 0, x.p_cap, x.p_common);
+  const int len = x.p_cap > 0 ? uni(x.p_lens[0]) : 0;
+  return x.p_sh.on ? rest_walk(len, x.p_cap) : seq_walk(len, x.p_cap, 1, 0, x.p_cap);
 }
 
 __device__ inline int wave_scan(int v, int lane) {
@@ -237,11 +239,12 @@ constexpr int HALF_TILE_ROWS = 16 * ROW_BYTES;
 __device__ inline int lane_key(int lane, int e) { return 4 * (lane >> 4) + (e & 3) + 16 * (e >> 2); }
 
 // Some value of the V tile is an infinity or NaN: the largest magnitude of its 16-bit numbers.
+template <int BYTES>
 __device__ inline bool tile_not_finite(const char *tV, int lane) {
   typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
   u16x8 most = 0;
 #pragma unroll
-  for (int i = 0; i < HALF_BYTES / 1024; ++i)
+  for (int i = 0; i < BYTES / 1024; ++i)
     most = __builtin_elementwise_max(most, *reinterpret_cast<const u16x8 *>(tV + i * 1024 + lane * 16) & (unsigned short)0x7fff);
   bool bad = false;
 #pragma unroll
@@ -270,40 +273,44 @@ struct CacheLogits {
 struct CacheMask {
   int n_init, n_local, first_pos, last_pos, n_tok;
   // every row sees every key of the tile
+  template <int TILE>
   __device__ inline bool whole(int kb) const {
-    return kb + CACHE_TILE - 1 <= first_pos && (kb + CACHE_TILE - 1 < n_init || last_pos - kb < n_local);
+    return kb + TILE - 1 <= first_pos && (kb + TILE - 1 < n_init || last_pos - kb < n_local);
   }
 };
 
 // O^T += V^T P^T for the tokens one by one, with the V rows that a token does not see as zeros: 0 * inf and
 // 0 * NaN of a slot that a row's mask excludes would otherwise reach the row.  Only tiles with a mask and
-// with such values take it, and only where there are several tokens: slots that no row sees are not loaded.  O goes through 8 KiB of LDS (`room`, the K tile that is no longer needed), so
-// that this rare path costs the others no registers.
-template <int NB>
-__device__ inline void update_by_token(CacheRows<NB> &st, const bf16x8 (&p)[NB][2], const char *tV, char *room, int kb,
+// with such values take it, and only where there are several tokens: slots that no row sees are not loaded.  O goes
+// through 4 KiB of LDS (`room`), half of its d at a time, so that this rare path costs the others no registers.
+// tV: 32 keys from kb on; P in PARTS parts.
+template <int NB, int PARTS>
+__device__ inline void update_by_token(CacheRows<NB> &st, const bf16x8 (&p)[NB][PARTS], const char *tV, char *room, int kb,
                                        const CacheMask &mask, int lane) {
   f32x4 *mine = reinterpret_cast<f32x4 *>(room) + lane;
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
+  for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-    for (int db = 0; db < 8; ++db) mine[64 * db] = st.o[nb][db];
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int db = 0; db < 4; ++db) mine[64 * db] = st.o[nb][4 * half + db];
 #pragma unroll 1
-    for (int i = 0; i < 8 * mask.n_tok; ++i) {
-      const int db = i & 7, t = i >> 3;
-      const int at = swz_byte(4 * (lane >> 4) + ((lane & 15) >> 2), 2 * db + ((lane & 3) >> 1)) + (lane & 1) * 8;
-      s16x8 w = __builtin_bit_cast(s16x8, lds_read_vt(tV, at, at + HALF_TILE_ROWS));
+      for (int i = 0; i < 4 * mask.n_tok; ++i) {
+        const int db = i & 3, t = i >> 2;
+        const int at = swz_byte(4 * (lane >> 4) + ((lane & 15) >> 2), 2 * (4 * half + db) + ((lane & 3) >> 1)) + (lane & 1) * 8;
+        s16x8 w = __builtin_bit_cast(s16x8, lds_read_vt(tV, at, at + HALF_TILE_ROWS));
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        w[e] = cache_visible(kb + lane_key(lane, e), mask.first_pos + t, mask.n_init, mask.n_local) ? w[e] : (short)0;
-      const bf16x8 a = __builtin_bit_cast(bf16x8, w);
-      f32x4 add = {0.f, 0.f, 0.f, 0.f};
-      add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][0], add, 0, 0, 0);
-      add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][1], add, 0, 0, 0);
-      if (st.tok[nb] == t) mine[64 * db] += add;
+        for (int e = 0; e < 8; ++e)
+          w[e] = cache_visible(kb + lane_key(lane, e), mask.first_pos + t, mask.n_init, mask.n_local) ? w[e] : (short)0;
+        const bf16x8 a = __builtin_bit_cast(bf16x8, w);
+        f32x4 add = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][part], add, 0, 0, 0);
+        if (st.tok[nb] == t) mine[64 * db] += add;
+      }
+#pragma unroll
+      for (int db = 0; db < 4; ++db) st.o[nb][4 * half + db] = mine[64 * db];
     }
-#pragma unroll
-    for (int db = 0; db < 8; ++db) st.o[nb][db] = mine[64 * db];
-  }
 }
 
 // A row's exponent reference is its maximum when it was last taken; logits may outgrow it by REF_ROOM (2^16 in
@@ -379,8 +386,8 @@ __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, cons
     st.l[nb] += sum;
   }
   wait_v();
-  if (EDGE && mask.n_tok > 1 && tile_not_finite(tV, lane)) {
-    update_by_token<NB>(st, p, tV, tK, kb, mask, lane);
+  if (EDGE && mask.n_tok > 1 && tile_not_finite<HALF_BYTES>(tV, lane)) {
+    update_by_token<NB, 2>(st, p, tV, tK, kb, mask, lane);
   } else {
 #pragma unroll
     for (int db = 0; db < 8; ++db) {
@@ -403,6 +410,24 @@ __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, cons
   }
 }
 
+// A lane's row of O that is final.
+template <int NB, class X>
+__device__ inline void store_row(X &x, const CachePart &c, const CacheRows<NB> &st, int nb, int row, float l, int lane) {
+  const LaneRow a = lane_row(x, c, row);
+  const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+  bf16_t *to = x.o + a.b * x.o_sb + (int64_t)(c.kvh * x.group + a.g) * x.o_sh + a.t * x.o_st + 4 * (lane >> 4);
+#pragma unroll
+  for (int db = 0; db < 8; ++db) {
+    const f32x4 r = st.o[nb][db] * inv;
+    const f32x2 u = {r[0], r[1]}, w = {r[2], r[3]};
+    uint2 two;
+    two.x = __builtin_bit_cast(unsigned, __builtin_convertvector(u, bf16x2));
+    two.y = __builtin_bit_cast(unsigned, __builtin_convertvector(w, bf16x2));
+    *reinterpret_cast<uint2 *>(to + 16 * db) = two;
+  }
+  if (x.stat && lane < 16) x.stat[((int64_t)c.b * x.n_kv + c.kvh) * x.rows + row] = float2{st.m[nb], l};
+}
+
 // End of a worker's part of a segment: rows of O that are final go out, others into the workspace.
 template <int NB, class X>
 __device__ inline void end_part(X &x, const CachePart &c, const CacheRows<NB> &st, bool whole, int slot, int lane) {
@@ -414,19 +439,7 @@ __device__ inline void end_part(X &x, const CachePart &c, const CacheRows<NB> &s
     l += __shfl_xor(l, 32);
     if (row >= rows) continue;
     if (whole && x.direct) {
-      const LaneRow a = lane_row(x, c, row);
-      const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
-      bf16_t *to = x.o + a.b * x.o_sb + (int64_t)(c.kvh * x.group + a.g) * x.o_sh + a.t * x.o_st + 4 * g;
-#pragma unroll
-      for (int db = 0; db < 8; ++db) {
-        const f32x4 r = st.o[nb][db] * inv;
-        const f32x2 u = {r[0], r[1]}, w = {r[2], r[3]};
-        uint2 two;
-        two.x = __builtin_bit_cast(unsigned, __builtin_convertvector(u, bf16x2));
-        two.y = __builtin_bit_cast(unsigned, __builtin_convertvector(w, bf16x2));
-        *reinterpret_cast<uint2 *>(to + 16 * db) = two;
-      }
-      if (x.stat && g == 0) x.stat[((int64_t)c.b * x.n_kv + c.kvh) * x.rows + row] = float2{st.m[nb], l};
+      store_row<NB>(x, c, st, nb, row, l, lane);
       continue;
     }
     const int64_t at = (int64_t)slot * x.slot_rows + nb * 16 + n;
@@ -517,16 +530,18 @@ struct CacheSource {
 #pragma unroll
     for (int half = 0; half < 2; ++half) rows16(h + (uint64_t)(unsigned)(kb + 16 * half) * rb, ofs, lds + 4096 * half);
   }
-  // ... row by row: slots that no row of the call sees are replaced by one that some row does
-  __device__ static inline void tile_in_part(const char *h, unsigned rb, int kb, const SeqWalk &w, unsigned lds, int lane) {
+  // BLOCKS times four rows of the tile at kb, from row `first` on, one by one: slots that no row of the call sees are
+  // replaced by one that some row does
+  template <int BLOCKS, class Walk>
+  __device__ static inline void rows_in_part(const char *h, unsigned rb, int kb, int first, const Walk &w, unsigned lds, int lane) {
     const int rl = lane >> 4, cpos = lane & 15;
 #pragma unroll
-    for (int blk = 0; blk < 8; ++blk) {
-      const int r = 4 * blk + rl;
+    for (int blk = 0; blk < BLOCKS; ++blk) {
+      const int r = first + 4 * blk + rl;
       int key = kb + r;
       if (key >= w.e1) key = max(key, w.lo);
       key = min(key, w.len - 1);
-      dma16(h + (uint64_t)(unsigned)key * rb + ((cpos ^ swz_f(r)) << 4), lds + blk * 1024);
+      dma16(h + (uint64_t)(unsigned)key * rb + ((cpos ^ swz_f(r)) << 4), lds + (first + 4 * blk) * ROW_BYTES);
     }
   }
   __device__ inline void fetch(int kb, const SeqWalk &w, unsigned lds, int lane) const {
@@ -535,8 +550,8 @@ struct CacheSource {
       tile(kh, k_rb, kofs, kb, lds);
       tile(vh, v_rb, vofs, kb, lds + HALF_BYTES);
     } else {
-      tile_in_part(kh, k_rb, kb, w, lds, lane);
-      tile_in_part(vh, v_rb, kb, w, lds + HALF_BYTES, lane);
+      rows_in_part<8>(kh, k_rb, kb, 0, w, lds, lane);
+      rows_in_part<8>(vh, v_rb, kb, 0, w, lds + HALF_BYTES, lane);
     }
   }
 };
@@ -627,7 +642,7 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
         if (more) MINF_WAIT_VMCNT(16); else MINF_WAIT_VMCNT(0);
       };
       char *tK = ring + slot;
-      if (mask.whole(kb)) cache_tile<NB, false>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
+      if (mask.whole<CACHE_TILE>(kb)) cache_tile<NB, false>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
       else cache_tile<NB, true>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
       __builtin_amdgcn_s_waitcnt(0xC07F);    // LDS reads done: the slot may be filled again
       slot ^= 2 * HALF_BYTES;
@@ -651,40 +666,64 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
   }
 }
 
-// ---- the slots that 33 to 128 rows see --------------------------------------------------------------------
-// Four waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile) and take 16 NB
-// rows each.  Memory bounds it still: 32 KiB a tile take a CU 1.4 us, the rows 0.5 (NB = 1) to 1.0 us.  (The 256-row
-// kernel, whose waves take 64 rows, runs 1.65 us a tile for any number of rows: 128 rows, 8 heads of 128K tokens,
-// 142 us.)  P in one bf16, as there: the matrix cores have no time to spare for its rest.
-// Order of the workgroups and layout of the results: as cache_common_kernel.
-template <int NB>
-__global__ __launch_bounds__(64 * CACHE_WAVES) void cache_shared_kernel(CacheCall x) {
+// ---- more than 32 rows -----------------------------------------------------------------------------------
+// Four waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile) and take 16 NB rows
+// each: 64 or 128 rows a workgroup.  Memory bounds it: 32 KiB a tile take a CU 1.4 us, about as long as the arithmetic of
+// 128 rows.  (128 rows, 8 heads of 128K tokens: 112 us; eight waves of 16 rows, which read every operand from LDS
+// twice as often, 132; the 256-row loop of cache_prefix_kernel 142.)  P in one bf16, as in the prefill kernels: the
+// matrix cores have no time to spare for its rest.
+// A workgroup takes one part (of x.*_sh.splits) of the tiles that its rows see; a segment in one part is final, of
+// others reference, sum and unnormalised O go to the workspace for cache_join_kernel.
+// Launch order: the row tiles that read the same slots run on one XCD, one after the other.
+constexpr int SHARED_RING = 4 * 2 * TILE_BYTES, SHARED_ROOM = 4096;        // ROOM (per wave): update_by_token
+template <int NB, bool PREFIX>
+__global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void cache_shared_kernel(CacheCall x) {
+  constexpr int W = CACHE_WAVES, prefix = PREFIX;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
-  const int per_xcd = blockIdx.x >> 3, rt = per_xcd % x.c_row_tiles;
-  const int group = (per_xcd / x.c_row_tiles) * 8 + (blockIdx.x & 7);          // (K/V head of a sequence, part of the slots)
-  const int heads = (x.p_common ? 1 : x.batch) * x.n_kv;
-  if (group >= heads * x.c_splits) return;
-  const int head = group / x.c_splits, part = group - head * x.c_splits;
+  const int lane = threadIdx.x & 63, wave = to_sgpr(threadIdx.x >> 6);
+  const SharedPart &sh = prefix ? x.p_sh : x.own_sh;
+  const int splits = sh.splits, tile_rows = 16 * NB * W;
+  const int per_xcd = blockIdx.x >> 3, turn = to_sgpr(per_xcd / sh.row_tiles), rt = per_xcd - turn * sh.row_tiles;
+  const int group = turn * 8 + (blockIdx.x & 7);                             // (K/V head of a sequence, part of the tiles)
+  const int heads = (prefix ? 1 : x.batch) * x.n_kv;
+  if (group >= heads * splits) return;
+  const int head = to_sgpr(group / splits), part = group - head * splits;
   CachePart c;
-  c.prefix = x.p_common;
-  c.b = c.prefix ? 0 : head / x.n_kv;
+  c.prefix = prefix;
+  c.b = prefix ? 0 : to_sgpr(head / x.n_kv);
   c.kvh = head - c.b * x.n_kv;
-  c.rt = rt * CACHE_WAVES + wave;                                              // row tile of 16 NB rows
-  const int len = uni(c.prefix ? x.p_lens[0] : x.lens[c.b]);
-  const int tiles = common_slots(min(max(len, 0), c.prefix ? x.p_cap : x.capacity) - (c.prefix ? 1 : x.n_new)) / COMMON_TILE;
-  const int per = common_share(tiles, x.c_splits), t0 = part * per, n = min(per, tiles - t0);
-  if (n <= 0) return;
+  c.rt = rt * W + wave;                                                      // row tile of 16 NB rows
+  const int last_row = min((rt + 1) * tile_rows, sh.rows) - 1;
+  const int len = to_sgpr(prefix ? x.p_lens[0] : x.lens[c.b]);
+  const TileWalk<SHARED_TILE> w = prefix ? tile_walk<SHARED_TILE>(len, x.p_cap, 1, 0, x.p_cap)
+                                         : rows_walk(rt * tile_rows, last_row, x.group, len, x.capacity, x.n_new, x.n_init, x.n_local);
+  const bool final = !prefix && x.direct && splits == 1;
+  const int per = to_sgpr(part_tiles(w.tiles, splits)), t0 = part * per, n = min(per, w.tiles - t0);
+  if (n <= 0 && !final) return;
 
+  CacheMask mask;
+  mask.n_init = prefix ? 0 : x.n_init;
+  mask.n_local = prefix ? x.p_cap : x.n_local;
+  mask.first_pos = prefix ? w.len - 1 : min(max(len, 0), x.capacity) - x.n_new + rt * tile_rows / x.group;
+  mask.last_pos = w.len - 1;
+  mask.n_tok = prefix ? 1 : last_row / x.group - rt * tile_rows / x.group + 1;
   CacheSource src;
-  src.strides(x, c.prefix, lane);
+  src.strides(x, prefix, lane);
   src.heads(x, c);
-  const unsigned ring = uni(lds_addr_of(lds)) + 4096 * wave;
-  auto fetch = [&](int t) {                                                    // this wave's 16 rows of K and V
-    const unsigned to = ring + (t & 3) * (2 * TILE_BYTES);
-    const int row = (t0 + min(t, n - 1)) * COMMON_TILE + 16 * wave;
-    src.rows16(src.kh + (uint64_t)(unsigned)row * src.k_rb, src.kofs, to);
-    src.rows16(src.vh + (uint64_t)(unsigned)row * src.v_rb, src.vofs, to + TILE_BYTES);
+  const unsigned ring = uni(lds_addr_of(lds));
+  constexpr int ROWS = 64 / W;                                               // of a tile, fetched by a wave
+  auto fetch = [&](int i) {
+    const unsigned to = ring + (i & 3) * (2 * TILE_BYTES);
+    const int kb = w.base(t0 + min(i, n - 1)), end = kb + SHARED_TILE;
+    if (end <= w.len && (kb >= w.lo || end <= w.e1)) {
+      const int row = kb + ROWS * wave;
+      const unsigned at = to_sgpr(to + 4096 * wave);
+      src.rows16(src.kh + (uint64_t)(unsigned)row * src.k_rb, src.kofs, at);
+      src.rows16(src.vh + (uint64_t)(unsigned)row * src.v_rb, src.vofs, at + TILE_BYTES);
+    } else {
+      src.template rows_in_part<ROWS / 4>(src.kh, src.k_rb, kb, ROWS * wave, w, to, lane);
+      src.template rows_in_part<ROWS / 4>(src.vh, src.v_rb, kb, ROWS * wave, w, to + TILE_BYTES, lane);
+    }
   };
   CacheRows<NB> st;
   load_queries<NB>(x, c, st.q, lane);
@@ -693,19 +732,30 @@ __global__ __launch_bounds__(64 * CACHE_WAVES) void cache_shared_kernel(CacheCal
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(st.q.q[nb][ks]));
-  fetch(0);
-  fetch(1);
-  fetch(2);
-  c.w = SeqWalk{};
-  begin_part<NB>(x, c, st, lane);
+  if (n > 0) {
+    fetch(0);
+    fetch(1);
+    fetch(2);
+  }
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int t = block_row<NB>(x, c, nb, lane).t;
+    st.tok[nb] = prefix ? 0 : t - rt * tile_rows / x.group;
+    st.pos[nb] = mask.first_pos + st.tok[nb];
+    st.m[nb] = -INFINITY;
+    st.l[nb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) st.o[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   CacheLane lo;
   lo.init(lane);
   const float c_log2 = x.c_log2;
-  for (int t = 0; t < n; ++t) {
-    MINF_WAIT_VMCNT(16);                       // this wave's part of tile t; those of t + 1 and t + 2 may run
-    __syncthreads();                           // all of tile t is there; all waves are done with tile t - 1
-    fetch(t + 3);                              // behind the last tile it is repeated: every tile issues 8 loads
-    const char *tK = lds + (t & 3) * (2 * TILE_BYTES), *tV = tK + TILE_BYTES;
+  for (int i = 0; i < n; ++i) {
+    MINF_WAIT_VMCNT(16);                       // this wave's part of tile i; those of i + 1 and i + 2 may run
+    __syncthreads();                           // all of tile i is there; all waves are done with tile i - 1
+    fetch(i + 3);                              // behind the last tile it is repeated: every tile issues as many loads
+    const char *tK = lds + (i & 3) * (2 * TILE_BYTES), *tV = tK + TILE_BYTES;
+    const int kb = w.base(t0 + i);
     f32x4 s[4][NB];                            // [16 keys][row block]
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt)
@@ -718,6 +768,15 @@ __global__ __launch_bounds__(64 * CACHE_WAVES) void cache_shared_kernel(CacheCal
           s[kt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, st.q.q[nb][ks], ks == 0 ? zero : s[kt][nb], 0, 0, 0);
         }
       }
+    const bool edge = !mask.whole<SHARED_TILE>(kb);
+    if (edge) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          s[e >> 2][nb][e & 3] = cache_visible(kb + 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3), st.pos[nb], mask.n_init, mask.n_local)
+                                     ? s[e >> 2][nb][e & 3] : -INFINITY;
+    }
     bool outgrown = false;
     float mx[NB];
 #pragma unroll
@@ -740,9 +799,10 @@ __global__ __launch_bounds__(64 * CACHE_WAVES) void cache_shared_kernel(CacheCal
         for (int db = 0; db < 8; ++db) st.o[nb][db] *= f;
       }
     }
+    const bool by_token = !PREFIX && edge && mask.n_tok > 1 && tile_not_finite<TILE_BYTES>(tV, lane);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      bf16x8 p[NB];
+      bf16x8 p[NB][1];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const float m = st.m[nb] == -INFINITY ? 0.f : st.m[nb];
@@ -753,32 +813,40 @@ __global__ __launch_bounds__(64 * CACHE_WAVES) void cache_shared_kernel(CacheCal
           const f32x2 v = {fast_exp2(fmaf(v4[e & 3], c_log2, -m)), fast_exp2(fmaf(v4[(e & 3) + 1], c_log2, -m))};
           sum += v[0] + v[1];
           const bf16x2 two = __builtin_convertvector(v, bf16x2);
-          p[nb][e] = two[0];
-          p[nb][e + 1] = two[1];
+          p[nb][0][e] = two[0];
+          p[nb][0][e + 1] = two[1];
         }
         st.l[nb] += sum;
+      }
+      if (by_token) {
+        update_by_token<NB, 1>(st, p, tV + half * HALF_BYTES, lds + SHARED_RING + wave * SHARED_ROOM, kb + CACHE_TILE * half, mask, lane);
+        continue;
       }
 #pragma unroll
       for (int db = 0; db < 8; ++db) {
         const int at = lo.v[db] + half * HALF_BYTES;
         const bf16x8 a = lds_read_vt(tV, at, at + HALF_TILE_ROWS);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb], st.o[nb][db], 0, 0, 0);
+        for (int nb = 0; nb < NB; ++nb) st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][0], st.o[nb][db], 0, 0, 0);
       }
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);        // LDS reads done
   }
   MINF_WAIT_VMCNT(0);                          // the repeated loads
-  const int64_t item = ((int64_t)head * x.c_row_tiles + rt) * x.c_splits + part;
+  const int64_t item = ((int64_t)head * sh.row_tiles + rt) * splits + part;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const int in_tile = (wave * NB + nb) * 16 + (lane & 15);
+    const int in_tile = (wave * NB + nb) * 16 + (lane & 15), row = rt * tile_rows + in_tile;
     float l = st.l[nb] + __shfl_xor(st.l[nb], 16);
     l += __shfl_xor(l, 32);
-    if (rt * x.c_tile_rows + in_tile >= x.c_rows) continue;
-    const int64_t at = item * x.c_tile_rows + in_tile;
-    if (lane < 16) x.common_ml[at] = float2{st.m[nb], l};
-    float *to = x.common_o + at * D + 4 * (lane >> 4);
+    if (row >= sh.rows) continue;
+    if (final) {
+      store_row<NB>(x, c, st, nb, row, l, lane);
+      continue;
+    }
+    const int64_t at = item * tile_rows + in_tile;
+    if (lane < 16) sh.ml[at] = float2{st.m[nb], l};
+    float *to = sh.o + at * D + 4 * (lane >> 4);
 #pragma unroll
     for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(to + 16 * db) = st.o[nb][db];
   }
@@ -817,7 +885,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
   const int b = seg / x.n_kv, kvh = seg - b * x.n_kv;
   const int mine = first_lens(x, lane);
   const SeqWalk pw = prefix_walk(x);
-  const int pre = pw.places() * x.n_kv * x.p_row_tiles;
+  const int pre = pw.places() * x.n_kv * x.p_row_tiles;                // row tiles of rows that are not the workers': 0
   const int heads = x.n_kv * x.row_tiles;
   int all, before;
   count_places(x, b, mine, lane, all, before);
@@ -882,23 +950,40 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
 
   const int row = item, t = row / x.group;
   const bool token = w.i0 + t >= 0;
-  const PieceList own = own_pieces(row);
-  if (x.direct && w.tiles > 0 && own.p.first == own.p.last) return;    // written by the worker itself
-  // the row's pieces in one list: of the common slots, the workers' of its own segment, of the prefix's
-  const int crow = x.p_common ? b * x.rows + row : row, n_own = w.tiles > 0 ? own.count() : 0;
-  const int64_t common0 = ((int64_t)(x.p_common ? kvh : seg) * x.c_row_tiles + crow / max(x.c_tile_rows, 1)) * x.c_splits;
-  int n_common = 0, n = 0;
+  const bool workers = !x.own_sh.on;
+  PieceList own = {};
+  if (workers) {
+    own = own_pieces(row);
+    if (x.direct && w.tiles > 0 && own.p.first == own.p.last) return;  // written by the worker itself
+  }
+  // The row's pieces in one list: of its own cache, then of the prefix, either the workers' or parts that several
+  // waves took together.
+  const SharedPart &osh = x.own_sh, &psh = x.p_sh;
+  const int prow = b * x.rows + row;
+  int64_t own0 = 0, pre0 = 0;
+  int n_own = 0, n_psh = 0, n = 0;
   PieceList pre_pieces = own;
   if (token) {
-    if (x.own_common) n_common = common_parts(w.s2 / COMMON_TILE, x.c_splits);
-    if (x.p_common) n_common = common_parts(pw.s2 / COMMON_TILE, x.c_splits);
-    n = n_common + n_own;
-    if (x.p_cap > 0 && pw.tiles > 0) {
-      const int prow = b * x.rows + row, prt = prow / tile_rows;
+    if (workers) {
+      n_own = w.tiles > 0 ? own.count() : 0;
+    } else {
+      const int rt = row / osh.tile_rows, r0 = rt * osh.tile_rows, r1 = min(r0 + osh.tile_rows, x.rows) - 1;
+      n_own = part_count(rows_walk(r0, r1, x.group, w.len, x.capacity, x.n_new, x.n_init, x.n_local).tiles, osh.splits);
+      own0 = ((int64_t)seg * osh.row_tiles + rt) * osh.splits * osh.tile_rows + (row - r0);
+    }
+    if (psh.on) {
+      const int rt = prow / psh.tile_rows, len = pw.len + (psh.tile_rows == 256 ? 0 : SHARED_TILE - 1);
+      n_psh = part_count(len / SHARED_TILE, psh.splits);
+      pre0 = ((int64_t)kvh * psh.row_tiles + rt) * psh.splits * psh.tile_rows + (prow - rt * psh.tile_rows);
+    }
+    n = n_own + n_psh;
+    if (x.p_row_tiles > 0 && pw.tiles > 0) {
+      const int prt = prow / tile_rows;
       pre_pieces.t0 = (kvh * x.p_row_tiles + prt) * pw.places() + SEGMENT_COST;
       pre_pieces.p = segment_pieces(pre_pieces.t0, pre_pieces.t0 + pw.tiles, share);
       pre_pieces.segment = kvh * x.p_row_tiles + prt;
       pre_pieces.base = prow - prt * tile_rows;
+      pre_pieces.share = share; pre_pieces.slot_rows = x.slot_rows; pre_pieces.workers = x.workers;
       n += pre_pieces.count();
     }
   }
@@ -910,11 +995,12 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
 #pragma unroll
     for (int j = 0; j < JOIN_AHEAD; ++j) {
       const int i = min(i0 + W * j, n - 1);
-      const bool c = i < n_common;
-      const int64_t at = c ? (common0 + i) * x.c_tile_rows + crow % max(x.c_tile_rows, 1)
-                           : i < n_common + n_own ? own.at(i - n_common) : pre_pieces.at(i - n_common - n_own);
-      ml[j] = (c ? x.common_ml : x.piece_ml)[at];
-      po[j] = *reinterpret_cast<const f32x2 *>((c ? x.common_o : x.piece_o) + at * D + 2 * lane);
+      const bool mine = i < n_own, shared = mine ? osh.on : i < n_own + n_psh;
+      const SharedPart &sh = mine ? osh : psh;
+      const int64_t at = mine ? (shared ? own0 + (int64_t)i * sh.tile_rows : own.at(i))
+                              : shared ? pre0 + (int64_t)(i - n_own) * sh.tile_rows : pre_pieces.at(i - n_own - n_psh);
+      ml[j] = (shared ? sh.ml : x.piece_ml)[at];
+      po[j] = *reinterpret_cast<const f32x2 *>((shared ? sh.o : x.piece_o) + at * D + 2 * lane);
     }
     float mx = m;
 #pragma unroll
@@ -1404,27 +1490,33 @@ static hipError_t launch_workers(const CacheCall &x, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int NB>
-static hipError_t launch_shared(const CacheCall &x, hipStream_t st) {
-  const size_t lds = 4 * 2 * TILE_BYTES;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_shared_kernel<NB>),
+template <int NB, bool PREFIX>
+static hipError_t launch_shared_as(const CacheCall &x, const SharedPart &sh, hipStream_t st) {
+  const size_t lds = SHARED_RING + CACHE_WAVES * SHARED_ROOM;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_shared_kernel<NB, PREFIX>),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  const int groups = (x.p_common ? 1 : x.batch) * x.n_kv * x.c_splits;
-  hipLaunchKernelGGL(cache_shared_kernel<NB>, dim3((groups + 7) / 8 * 8 * x.c_row_tiles), dim3(64 * CACHE_WAVES), lds, st, x);
+  const int groups = (PREFIX ? 1 : x.batch) * x.n_kv * sh.splits;
+  hipLaunchKernelGGL((cache_shared_kernel<NB, PREFIX>), dim3((groups + 7) / 8 * 8 * sh.row_tiles), dim3(64 * CACHE_WAVES), lds, st, x);
   return hipGetLastError();
+}
+template <bool PREFIX>
+static hipError_t launch_shared(const CacheCall &x, const SharedPart &sh, hipStream_t st) {
+  if (!sh.on) return hipSuccess;
+  if (sh.tile_rows == 256) return launch_cache_prefix(x, st);
+  return sh.tile_rows == 64 ? launch_shared_as<1, PREFIX>(x, sh, st) : launch_shared_as<2, PREFIX>(x, sh, st);
 }
 
 hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
-  hipError_t e = hipSuccess;
-  if (x.p_common || x.own_common)
-    e = x.c_tile_rows == 64 ? launch_shared<1>(x, st) : x.c_tile_rows == 128 ? launch_shared<2>(x, st) : launch_cache_common(x, st);
+  hipError_t e = launch_shared<true>(x, x.p_sh, st);
+  if (e == hipSuccess) e = launch_shared<false>(x, x.own_sh, st);
+  if (e == hipSuccess && (x.row_tiles > 0 || x.p_row_tiles > 0)) e = x.row_blocks == 1 ? launch_workers<1>(x, st) : launch_workers<2>(x, st);
   if (e != hipSuccess) return e;
-  e = x.row_blocks == 1 ? launch_workers<1>(x, st) : launch_workers<2>(x, st);
-  if (e != hipSuccess) return e;
+  const bool final = x.direct && x.own_sh.on && x.own_sh.splits == 1;  // nothing to join
   // Four waves per row while that is a round of the chip's waves or less
   const int rows = x.batch * x.n_kv * x.rows, weigh = x.logits ? x.batch * x.n_kv * ((x.capacity + 1023) / 1024) : 0;
-  if (rows <= 1024) {
+  if (final) {
+  } else if (rows <= 1024) {
     hipLaunchKernelGGL(cache_join_kernel<4>, dim3(rows + weigh), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks, rows);
   } else {
     const int joins = (rows + JOIN_WAVES - 1) / JOIN_WAVES;

@@ -17,46 +17,63 @@
 
 namespace minf {
 
-constexpr int CACHE_TILE = 32, COMMON_TILE = 64;
+constexpr int CACHE_TILE = 32, SHARED_TILE = 64;
 // A segment (below) costs a worker its tiles and, for its rows and its result, as much as two more: it takes up so
 // many places more in the list, in front of its tiles.
 constexpr int SEGMENT_COST = 2;
 
 // Tiles of one sequence: T1 tiles of the sink from slot 0 on, then the window's from slot s2 (a multiple of
 // the tile) on.  Sink and window that touch in a tile are walked as one (T1 = 0, s2 = 0).
-struct SeqWalk {
+template <int TILE>
+struct TileWalk {
   int32_t len, i0, T1, s2, tiles;       // i0: position of the first of the n_new rows (negative: no token)
   int32_t e1, lo;                       // some row sees the slots 0 .. e1 - 1 and lo .. len - 1, no row another one
   MINF_HD int32_t places() const { return tiles > 0 ? tiles + SEGMENT_COST : 0; }
-  MINF_HD int32_t base(int32_t t) const { return t < T1 ? t * CACHE_TILE : s2 + (t - T1) * CACHE_TILE; }
+  MINF_HD int32_t base(int32_t t) const { return t < T1 ? t * TILE : s2 + (t - T1) * TILE; }
   // tile that holds a slot, or -1
   MINF_HD int32_t tile_of(int32_t slot) const {
-    if (slot < T1 * CACHE_TILE) return slot / CACHE_TILE;
-    return slot >= s2 && slot < len ? T1 + (slot - s2) / CACHE_TILE : -1;
+    if (slot < T1 * TILE) return slot / TILE;
+    return slot >= s2 && slot < len ? T1 + (slot - s2) / TILE : -1;
   }
 };
+typedef TileWalk<CACHE_TILE> SeqWalk;
 
-// n_init, n_local: at most the capacity, so that no sum here leaves 32 bits.  behind_common: only what lies behind
-// the slots that every row sees, in whole tiles of 64 (n_local: the capacity); those are another kernel's.
-MINF_HD int32_t common_slots(int32_t i0) { return i0 < 0 ? 0 : (i0 + 1) / COMMON_TILE * COMMON_TILE; }
-MINF_HD SeqWalk seq_walk(int32_t len, int32_t capacity, int32_t n_new, int32_t n_init, int32_t n_local,
-                         bool behind_common = false) {
-  SeqWalk w;
+// n_init, n_local: at most the capacity, so that no sum here leaves 32 bits.
+template <int TILE>
+MINF_HD TileWalk<TILE> tile_walk(int32_t len, int32_t capacity, int32_t n_new, int32_t n_init, int32_t n_local) {
+  TileWalk<TILE> w;
   w.len = len < 0 ? 0 : (len > capacity ? capacity : len);
   w.i0 = w.len - n_new;
-  if (behind_common) {
-    w.e1 = w.T1 = 0;
-    w.lo = w.s2 = common_slots(w.i0);
-    w.tiles = (w.len - w.s2 + CACHE_TILE - 1) / CACHE_TILE;
-    return w;
-  }
   w.e1 = n_init < w.len ? n_init : w.len;
   w.lo = w.i0 - n_local + 1;
   if (w.lo < 0) w.lo = 0;
-  w.s2 = w.lo / CACHE_TILE * CACHE_TILE;
-  w.T1 = (w.e1 + CACHE_TILE - 1) / CACHE_TILE;
-  if (w.s2 <= w.T1 * CACHE_TILE) w.s2 = w.T1 = 0;
-  w.tiles = w.T1 + (w.len - w.s2 + CACHE_TILE - 1) / CACHE_TILE;
+  w.s2 = w.lo / TILE * TILE;
+  w.T1 = (w.e1 + TILE - 1) / TILE;
+  if (w.s2 <= w.T1 * TILE) w.s2 = w.T1 = 0;
+  w.tiles = w.T1 + (w.len - w.s2 + TILE - 1) / TILE;
+  return w;
+}
+MINF_HD SeqWalk seq_walk(int32_t len, int32_t capacity, int32_t n_new, int32_t n_init, int32_t n_local) {
+  return tile_walk<CACHE_TILE>(len, capacity, n_new, n_init, n_local);
+}
+
+// What is left of a prefix of len slots behind its whole tiles of 64.
+MINF_HD SeqWalk rest_walk(int32_t len, int32_t capacity) {
+  SeqWalk w = seq_walk(len, capacity, 1, 0, capacity);
+  w.lo = w.s2 = w.len / SHARED_TILE * SHARED_TILE;
+  w.e1 = w.T1 = 0;
+  w.tiles = (w.len - w.s2 + CACHE_TILE - 1) / CACHE_TILE;
+  return w;
+}
+
+// The rows first .. last of a sequence (row r is token r / group of its n_new): what they see.
+MINF_HD TileWalk<SHARED_TILE> rows_walk(int32_t first, int32_t last, int32_t group, int32_t len, int32_t capacity, int32_t n_new,
+                                        int32_t n_init, int32_t n_local) {
+  len = len < 0 ? 0 : (len > capacity ? capacity : len);
+  const int32_t t0 = first / group, t1 = last / group;
+  int32_t end = len - n_new + t1 + 1;
+  if (end < 0) end = 0;
+  TileWalk<SHARED_TILE> w = tile_walk<SHARED_TILE>(end, capacity, t1 - t0 + 1, n_init, n_local);
   return w;
 }
 
@@ -105,10 +122,10 @@ MINF_HD int32_t piece_slot(int32_t worker, int32_t t0, int32_t share) {
   return 2 * worker + (t0 > worker * share ? 1 : 0);
 }
 
-// The common slots of a segment are cut into at most `splits` parts of equally many tiles: tiles per part.
-MINF_HD int32_t common_share(int32_t tiles, int32_t splits) { return (tiles + splits - 1) / splits; }
-MINF_HD int32_t common_parts(int32_t tiles, int32_t splits) {
-  const int32_t per = common_share(tiles, splits);
+// Tiles that four waves take together are cut into at most `splits` parts of equally many: tiles per part.
+MINF_HD int32_t part_tiles(int32_t tiles, int32_t splits) { return (tiles + splits - 1) / splits; }
+MINF_HD int32_t part_count(int32_t tiles, int32_t splits) {
+  const int32_t per = part_tiles(tiles, splits);
   return per > 0 ? (tiles + per - 1) / per : 0;
 }
 

@@ -221,6 +221,13 @@ hipError_t launch_build_bs(const QKV &x, int nb, const HeadList &hl, int topk, i
 
 // ---- the cache calls (cache_kernels.hip) --------------------------------------------------------------------
 // Pointers of device memory, strides in elements (_sb: sequence, _sh: head, _st: token).
+// Rows that four waves take together, tile_rows at a time, their tiles cut into `splits` parts: 64 or 128 of them
+// cache_shared_kernel, 256 cache_prefix_kernel (of a prefix, its whole tiles of 64; the rest is the workers').
+struct SharedPart {
+  int32_t on, rows, tile_rows, row_tiles, splits;
+  float2 *ml;                           // [K/V head (of a sequence), row_tiles][splits][tile_rows]: reference, sum
+  float *o;                             // ... [128]
+};
 struct CacheCall {
   const bf16_t *q, *k, *v, *pk, *pv;    // pk, pv: the shared prefix, or NULL
   bf16_t *o;
@@ -232,21 +239,17 @@ struct CacheCall {
   int32_t rows, row_tiles;              // rows of a K/V head (group * n_new), in tiles of 16 row_blocks
   int32_t p_cap, p_row_tiles;           // capacity of the prefix (0: none), row tiles of its batch * rows rows
   int32_t row_blocks, workers, max_tiles, slot_rows;
-  // The slots that every row sees, in whole tiles of 64, are taken by cache_shared_kernel (64 or 128 rows at a
-  // time) or cache_common_kernel (256): of the prefix (p_common) or of every sequence (own_common); the workers take
-  // the rest.  direct: workers may write O themselves.
-  int32_t p_common, own_common, c_rows, c_tile_rows, c_row_tiles, c_splits, direct;
+  SharedPart own_sh, p_sh;              // more than 32 rows: not for the workers
+  int32_t direct;                       // O of a whole segment is final (no prefix)
   float c_log2;
   // workspace
   float *logits;                        // [sequence, K/V head, max_tiles][rows][32], base 2; NULL: not kept
   float2 *stat;                         // [sequence, K/V head, rows]: reference, sum; NULL: no weights
   float2 *piece_ml;                     // [2 workers + segments][slot_rows]: reference, sum
   float *piece_o;                       // [2 workers + segments][slot_rows][128]
-  float2 *common_ml;                    // [K/V head (of a sequence), c_row_tiles][c_splits][c_tile_rows]
-  float *common_o;                      // [K/V head (of a sequence), c_row_tiles][c_splits][c_tile_rows][128]
 };
 hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st);
-hipError_t launch_cache_common(const CacheCall &x, hipStream_t st);     // attn_kernels.hip
+hipError_t launch_cache_prefix(const CacheCall &x, hipStream_t st);     // attn_kernels.hip
 
 struct SelectState {
   uint32_t key;

@@ -48,7 +48,7 @@ def attention(q, k, v, n, n_init, n_local, scale=None, pk=None, pv=None):
 
 
 P_TWO_BF16 = 2.0 ** -16    # P as the sum of two bf16: what is left of p after one half step is rounded again
-P_BF16 = 2.0 ** -8         # P as one bf16 (slots that more than 32 rows see): off by half a step, 2^-8 of the value
+P_BF16 = 2.0 ** -8         # P as one bf16 (more than 32 rows of a K/V head): off by half a step, 2^-8 of the value
 
 
 def check_o(got, want, mag, slack, what="", p_step=P_TWO_BF16):

@@ -55,24 +55,43 @@ static int walks() {
   return cases;
 }
 
-// Behind the common slots: the tiles and they together hold every slot once, and every row sees all common ones.
-static int common() {
+// Row tiles: the walk of some rows of a sequence holds every slot that one of them sees once, and parts hold
+// every tile once.
+static int rows() {
   int cases = 0;
-  for (int cap : {1, 64, 65, 200, 1000})
+  for (int cap : {1, 64, 65, 200, 700})
     for (int T : {1, 2, 40, 64})
-      for (int len = 0; len <= cap; len += (cap > 100 ? 13 : 1)) {
-        ++cases;
-        const SeqWalk w = seq_walk(len, cap, T, 0, cap, true);
-        const int c = common_slots(w.i0);
-        CHECK(c % 64 == 0 && c >= 0 && c <= len && w.base(0) == c);
-        CHECK(c == 0 || c - 1 <= w.i0);
-        CHECK(c + w.tiles * CACHE_TILE >= len && c + (w.tiles - 1) * CACHE_TILE < len + (len == 0));
-        CHECK((w.len - c) <= T + 63);
-        for (int splits : {1, 2, 7, 64}) {
-          const int tiles = c / 64, per = common_share(tiles, splits), parts = common_parts(tiles, splits);
-          CHECK(parts <= splits && parts * per >= tiles && (tiles == 0 ? parts == 0 : (parts - 1) * per < tiles));
-        }
-      }
+      for (int group : {1, 3, 8})
+        for (int tile_rows : {64, 128, 256})
+          for (int ni : {0, 5, 100})
+            for (int nl : {1, 50, 700}) {
+              if (ni > cap || nl > cap) continue;
+              for (int len = 0; len <= cap; len += (cap > 100 ? 37 : 1))
+                for (int r0 = 0; r0 < T * group; r0 += tile_rows) {
+                  ++cases;
+                  const int r1 = (r0 + tile_rows < T * group ? r0 + tile_rows : T * group) - 1;
+                  const auto w = rows_walk(r0, r1, group, len, cap, T, ni, nl);
+                  const int i0 = len - T;
+                  std::vector<int> times(cap + SHARED_TILE, 0);
+                  for (int t = 0; t < w.tiles; ++t) {
+                    CHECK(w.base(t) >= 0 && w.base(t) < len && w.base(t) % SHARED_TILE == 0);
+                    for (int i = 0; i < SHARED_TILE; ++i) ++times[w.base(t) + i];
+                  }
+                  for (int j = 0; j < cap; ++j) {
+                    bool seen = false;
+                    for (int t = r0 / group; t <= r1 / group; ++t) seen = seen || (i0 + t >= 0 && cache_visible(j, i0 + t, ni, nl));
+                    CHECK(times[j] <= 1 && (!seen || times[j] == 1));
+                    CHECK(!seen || (j < w.len && (j < w.e1 || j >= w.lo)));
+                  }
+                  // the position of the first row's token where it is one
+                  CHECK(i0 + r1 / group < 0 || w.i0 == i0 + r0 / group);
+                  CHECK(i0 + r1 / group >= 0 || w.tiles == 0);
+                  for (int splits : {1, 2, 7, 64}) {
+                    const int per = part_tiles(w.tiles, splits), parts = part_count(w.tiles, splits);
+                    CHECK(parts <= splits && parts * per >= w.tiles && (w.tiles == 0 ? parts == 0 : (parts - 1) * per < w.tiles));
+                  }
+                }
+            }
   return cases;
 }
 
@@ -118,7 +137,12 @@ static int shares() {
 }
 
 int main() {
-  const int a = walks(), b = shares(), c = common();
-  if (fails == 0) printf("ok walks %d shares %d common %d\n", a, b, c);
+  for (int len = 0; len <= 300; ++len) {                         // the rest of a prefix behind its whole tiles
+    const SeqWalk w = rest_walk(len, 300);
+    CHECK(w.s2 == len / 64 * 64 && w.tiles == (len % 64 + 31) / 32 && w.T1 == 0 && w.e1 == 0 && w.lo == w.s2 && w.len == len);
+    CHECK(w.tiles == 0 || (w.base(0) == w.s2 && w.base(w.tiles - 1) < len && w.i0 == len - 1));
+  }
+  const int a = walks(), b = shares(), c = rows();
+  if (fails == 0) printf("ok walks %d shares %d rows %d\n", a, b, c);
   return fails != 0;
 }

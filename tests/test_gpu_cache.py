@@ -58,9 +58,9 @@ def check_attention(q, cache, o, n_init=0, n_local=BIG, scale=None, prefix=None,
         P = int(prefix.lens[0])
         pk, pv = R.f64(prefix.k)[0][:, :P], R.f64(prefix.v)[0][:, :P]
     cap = kd.shape[2]
-    # slots that more than 32 rows of a K/V head see are multiplied with P in one bf16
+    # more than 32 rows of a K/V head are multiplied with P in one bf16
     rows = q.shape[1] // kd.shape[1] * q.shape[2]
-    many = rows * len(qd) > 32 if prefix is not None else rows > 32 and n_local >= cap
+    many = rows * (1 if prefix is None else len(qd)) > 32
     for b, n in enumerate(cache.lens.tolist()):
         n = max(0, min(n, cap))
         want, w, mag, slack = R.attention(qd[b], kd[b], vd[b], n, n_init, n_local, scale, pk, pv)
