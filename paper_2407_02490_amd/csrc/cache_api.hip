@@ -221,7 +221,7 @@ minf_status run_plan(const minf_queries *q, const minf_kv_cache *c, const minf_k
   return launch_cache_attn(p.x, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? MINF_OK : MINF_ERR_HIP;
 }
 
-// The selection's cut and workspace.  Rows of up to 16K slots: one workgroup per row.  Longer ones in chunks of
+// The selection's cut and workspace.  Rows of up to 32K slots: one workgroup per row.  Longer ones in chunks of
 // 4096 to 32768 slots (a chunk's counts are 16-bit numbers), small enough for one workgroup per CU.
 struct EvictPlan {
   int32_t chunks, chunk_slots;
@@ -233,7 +233,7 @@ EvictPlan evict_plan(int64_t rows, int64_t capacity) {
   p.chunks = 0;
   p.chunk_slots = 0;
   p.at_hist = p.at_state = p.need = up(rows * sizeof(int32_t));
-  if (capacity <= 16384) return p;
+  if (capacity <= 32768) return p;
   int64_t slots = (rows * capacity / CUS + 1023) / 1024 * 1024;
   slots = slots < 4096 ? 4096 : slots > 32768 ? 32768 : slots;
   p.chunk_slots = (int32_t)slots;

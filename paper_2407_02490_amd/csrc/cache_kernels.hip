@@ -873,7 +873,8 @@ struct PieceList {
   }
 };
 
-template <int W>
+// SHARED: with rows that several waves took together (without them the code is smaller, which a short call notices).
+template <int W, bool SHARED>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x, int tile_rows, int joins) {
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   const bool joining = (int)blockIdx.x < joins;
@@ -950,7 +951,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
 
   const int row = item, t = row / x.group;
   const bool token = w.i0 + t >= 0;
-  const bool workers = !x.own_sh.on;
+  const bool workers = !SHARED || !x.own_sh.on;
   PieceList own = {};
   if (workers) {
     own = own_pieces(row);
@@ -971,7 +972,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
       n_own = part_count(rows_walk(r0, r1, x.group, w.len, x.capacity, x.n_new, x.n_init, x.n_local).tiles, osh.splits);
       own0 = ((int64_t)seg * osh.row_tiles + rt) * osh.splits * osh.tile_rows + (row - r0);
     }
-    if (psh.on) {
+    if (SHARED && psh.on) {
       const int rt = prow / psh.tile_rows, len = pw.len + (psh.tile_rows == 256 ? 0 : SHARED_TILE - 1);
       n_psh = part_count(len / SHARED_TILE, psh.splits);
       pre0 = ((int64_t)kvh * psh.row_tiles + rt) * psh.splits * psh.tile_rows + (prow - rt * psh.tile_rows);
@@ -995,7 +996,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
 #pragma unroll
     for (int j = 0; j < JOIN_AHEAD; ++j) {
       const int i = min(i0 + W * j, n - 1);
-      const bool mine = i < n_own, shared = mine ? osh.on : i < n_own + n_psh;
+      const bool mine = i < n_own, shared = SHARED && (mine ? osh.on : i < n_own + n_psh);
       const SharedPart &sh = mine ? osh : psh;
       const int64_t at = mine ? (shared ? own0 + (int64_t)i * sh.tile_rows : own.at(i))
                               : shared ? pre0 + (int64_t)(i - n_own) * sh.tile_rows : pre_pieces.at(i - n_own - n_psh);
@@ -1515,12 +1516,14 @@ hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
   const bool final = x.direct && x.own_sh.on && x.own_sh.splits == 1;  // nothing to join
   // Four waves per row while that is a round of the chip's waves or less
   const int rows = x.batch * x.n_kv * x.rows, weigh = x.logits ? x.batch * x.n_kv * ((x.capacity + 1023) / 1024) : 0;
-  if (final) {
-  } else if (rows <= 1024) {
-    hipLaunchKernelGGL(cache_join_kernel<4>, dim3(rows + weigh), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks, rows);
-  } else {
-    const int joins = (rows + JOIN_WAVES - 1) / JOIN_WAVES;
-    hipLaunchKernelGGL(cache_join_kernel<1>, dim3(joins + weigh), dim3(64 * JOIN_WAVES), 0, st, x, 16 * x.row_blocks, joins);
+  if (!final) {
+    const bool four = rows <= 1024;
+    const int joins = four ? rows : (rows + JOIN_WAVES - 1) / JOIN_WAVES, tile_rows = 16 * x.row_blocks;
+    auto join = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(joins + weigh), dim3(64 * JOIN_WAVES), 0, st, x, tile_rows, joins);
+    };
+    if (x.own_sh.on || x.p_sh.on) four ? join(cache_join_kernel<4, true>) : join(cache_join_kernel<1, true>);
+    else four ? join(cache_join_kernel<4, false>) : join(cache_join_kernel<1, false>);
   }
   if ((e = hipGetLastError()) != hipSuccess || !x.weight || x.logits) return e;
   hipLaunchKernelGGL(cache_column_kernel, dim3((x.capacity + COLUMN_KEYS - 1) / COLUMN_KEYS, x.n_kv, x.batch), dim3(256), 0, st, x);
