@@ -265,13 +265,14 @@ minf_status minf_dense_attn(const minf_qkv *x, const int32_t *heads, int32_t n_h
  *   weight  [batch, n_kv_heads, capacity] fp32, slots contiguous, or NULL:
  *           attention weight that every slot has received
  *
- * General rules as above, with these differences: capacity and lens need not
- * be multiples of anything; the calls take every head of the layer; the
- * sequences of a batch may run at the same time in any order.  A value in a slot
- * that the mask hides from a row (NaN and infinities too) does not reach that
- * row.  Results are the same bits from call to call; the sums of a sequence are
- * cut by the lengths of the whole batch, so that its bits may differ in another
- * batch.
+ * General rules as above, with these differences: capacity (up to 2^29) and
+ * lens need not be multiples of anything; the calls take every head of the
+ * layer.  A value in a slot that the mask hides from a row (NaN and infinities
+ * too) does not reach that row.  Logits, sums and O are fp32; the probabilities
+ * multiply V as two bf16 (high and low part), those of more than 32 rows per K/V
+ * head (for a prefix: of the batch) as one, as in the prefill.  Results are the
+ * same bits from call to call; where a sequence's sums are cut depends on the
+ * whole batch, so that its bits may differ in another one.
  */
 #define MINF_MAX_NEW 64   /* new tokens per call and sequence */
 
@@ -288,9 +289,11 @@ typedef struct {
  * Query rows of the n_new newest tokens of every sequence: q, o [batch,
  * n_q_heads, n_new, head_dim] bf16.  Row t of sequence b stands at position
  * lens[b] - n_new + t (its own key is in the cache already); where that is
- * negative there is no token, and the row gives zeros.  o may be q itself;
- * otherwise it must not lie over anything the call reads, and no two of its
- * rows over each other (MINF_ERR_SHAPE for strides that make them).
+ * negative there is no token, and the row gives zeros.  o may be q itself
+ * (but for weights of more than 16 rows per K/V head, which are computed from q
+ * after o); otherwise it must not lie over anything the call reads, and no two
+ * of its rows over each other (MINF_ERR_SHAPE, also where the library cannot
+ * tell: it compares addresses, strides and sizes).
  */
 typedef struct {
   const void *q;
@@ -306,10 +309,11 @@ typedef enum {
   MINF_WEIGHTS_ADD = 2    /* weight[b, h, j] += sum of p_ij                        */
 } minf_weights;
 
-/* Workspace sizes in bytes (0 on invalid arguments).  With weights the logits are kept, 4 bytes
- * per query row and visible key; without them the size depends on the rows alone.  ws must be
- * 256-byte aligned; its contents mean nothing before and after a call.  Calls that may overlap in
- * time need a workspace each. */
+/* Workspace sizes in bytes (0 on invalid arguments).  They depend on shapes and masks, not on lens.
+ * Weights of up to 16 query rows per K/V head keep the logits, 4 bytes per row and key that the mask
+ * may show.  An eviction takes 12 KiB per 4096 to 32768 slots of a K/V head (none up to a capacity of
+ * 32768) and 4 bytes per head.  ws must be 256-byte aligned; its contents mean nothing before and
+ * after a call.  Calls that may overlap in time need a workspace each. */
 size_t minf_cache_attn_workspace_bytes(const minf_queries *x, const minf_kv_cache *cache, int32_t n_init,
                                        int32_t n_local, int32_t weights);
 size_t minf_prefix_attn_workspace_bytes(const minf_queries *x, const minf_kv_cache *prefix,
@@ -325,7 +329,8 @@ size_t minf_cache_evict_workspace_bytes(const minf_kv_cache *cache, int32_t keep
  * weights: with MINF_WEIGHTS_SET or _ADD the call also gives every slot j <
  * lens[b] of cache->weight the attention weight p_ij it received in this call,
  * summed over the rows and the query heads of the K/V head's group (0 for slots
- * that no row sees).  fp32 logits and sums in a fixed order.
+ * that no row sees); the slots behind are left as they are.  The weights may not
+ * lie over k, v, q, o or lens.
  */
 minf_status minf_cache_attn(const minf_queries *x, const minf_kv_cache *cache, int32_t n_init, int32_t n_local,
                             int32_t weights, void *ws, size_t ws_bytes, void *hip_stream);
@@ -352,9 +357,9 @@ minf_status minf_prefix_attn(const minf_queries *x, const minf_kv_cache *prefix,
  * ascending, -1 behind them.
  * `to` is either the cache itself (the same k, v, weight and strides: eviction
  * in place) or memory that none of the cache's k, v and weight lies in; to->lens
- * may be cache->lens.  to->batch and to->n_kv_heads as in the cache, to->capacity
- * >= keep (in place: the cache's); n_init, n_recent >= 0, 1 <= keep, n_init +
- * n_recent <= keep.
+ * may be cache->lens.  K, V and weight of `to` must be apart.  to->batch and
+ * to->n_kv_heads as in the cache, to->capacity >= keep (in place: the cache's);
+ * n_init, n_recent >= 0, 1 <= keep, n_init + n_recent <= keep.
  */
 minf_status minf_cache_evict(const minf_kv_cache *cache, int32_t n_init, int32_t n_recent, int32_t keep,
                              const minf_kv_cache *to, int32_t *kept, void *ws, size_t ws_bytes, void *hip_stream);

@@ -435,7 +435,8 @@ def minf_cache_evict_workspace_bytes(cache, keep):
 
 def minf_cache_attn(q, o, cache, ws, n_init=0, n_local=None, weights=None, scale=0.0, stream=None):
     """o = attention of the newest tokens q against the cache, sink + sliding window (n_local=None: the
-    whole cache); weights="set" / "add": cache.weight receives the attention weight of every slot."""
+    whole cache); weights="set" / "add": cache.weight receives the attention weight of every slot.
+    o may be q (not with weights of more than 16 rows per K/V head)."""
     _cache_call(lib().minf_cache_attn, cache, ws, stream, ctypes.byref(_queries(q, o, cache, scale)), cache._ref, n_init,
                 cache.capacity if n_local is None else n_local, _weights(weights))
 

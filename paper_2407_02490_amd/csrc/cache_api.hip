@@ -12,6 +12,7 @@ using namespace minf;
 namespace {
 
 constexpr int CUS = 256;
+constexpr int32_t MAX_CAPACITY = 1 << 29;              // positions, and sums of a few of them, in 32 bits
 constexpr int64_t MAX_BLOCKS = (1 << 24) - 1;          // of 256 threads, in one grid dimension
 
 bool stride_ok(const int64_t (&s)[3], int head_dim) {
@@ -43,7 +44,7 @@ Range v_range(const minf_kv_cache *c) { return range_of(rows_of(c->v, c->v_strid
 minf_status check_cache(const minf_kv_cache *c, bool need_weight, bool written) {
   if (!c || !c->k || !c->v || !c->lens || (need_weight && !c->weight)) return MINF_ERR_NULL;
   if (c->head_dim != 128) return MINF_ERR_SHAPE;
-  if (c->batch < 1 || c->n_kv_heads < 1 || c->capacity < 1) return MINF_ERR_SHAPE;
+  if (c->batch < 1 || c->n_kv_heads < 1 || c->capacity < 1 || c->capacity > MAX_CAPACITY) return MINF_ERR_SHAPE;
   if ((int64_t)c->batch * c->n_kv_heads > 65535) return MINF_ERR_SHAPE;
   if (!stride_ok(c->k_stride, 128) || !stride_ok(c->v_stride, 128) || !aligned16(c->k) || !aligned16(c->v)) return MINF_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(c->lens) % 4 != 0) return MINF_ERR_SHAPE;
@@ -181,12 +182,18 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   return MINF_OK;
 }
 
-// o over something that other workgroups still read.
-bool o_meets_inputs(const minf_queries *q, const minf_kv_cache *c, const minf_kv_cache *prefix, bool weight) {
+// o over something that other workgroups still read, or weights over an input.  (o in the place of q: a workgroup reads
+// its rows before it writes them; but the weights of more than 16 rows per K/V head are computed from q afterwards.)
+bool outputs_meet_inputs(const minf_queries *q, const minf_kv_cache *c, const minf_kv_cache *prefix, bool weight) {
   const BatchLayout lo = rows_of(q->o, q->o_stride, c->batch, q->n_q_heads, q->n_new);
   const BatchLayout lq = rows_of(q->q, q->q_stride, c->batch, q->n_q_heads, q->n_new);
   const Range o = range_of(lo);
-  const bool in_place = lo.base == lq.base && lo.sb == lq.sb && lo.sh == lq.sh && lo.st == lq.st;
+  const bool again = weight && q->n_q_heads / c->n_kv_heads * q->n_new > 16;
+  const bool in_place = !again && lo.base == lq.base && lo.sb == lq.sb && lo.sh == lq.sh && lo.st == lq.st;
+  if (weight) {
+    const Range w = weight_range(c);
+    if (w.meets(k_range(c)) || w.meets(v_range(c)) || w.meets(range_of(lq)) || w.meets(lens_range(c->lens, c->batch))) return true;
+  }
   auto apart = [&](const void *p, const int64_t (&s)[3], int batch, int heads, int tokens) {
     return input_apart(lo, rows_of(p, s, batch, heads, tokens));
   };
@@ -204,7 +211,7 @@ minf_status run_plan(const minf_queries *q, const minf_kv_cache *c, const minf_k
   Plan p;
   const minf_status s = make_plan(q, c, prefix, n_init, n_local, weights, true, p);
   if (s != MINF_OK) return s;
-  if (o_meets_inputs(q, c, prefix, weights != MINF_WEIGHTS_NONE)) return MINF_ERR_SHAPE;
+  if (outputs_meet_inputs(q, c, prefix, weights != MINF_WEIGHTS_NONE)) return MINF_ERR_SHAPE;
   if (!ws || ws_bytes < p.need || reinterpret_cast<uintptr_t>(ws) % 256 != 0) return MINF_ERR_WORKSPACE;
   char *w = static_cast<char *>(ws);
   p.x.piece_o = reinterpret_cast<float *>(w);
@@ -286,6 +293,10 @@ minf_status minf_cache_evict(const minf_kv_cache *cache, int32_t n_init, int32_t
   if (to->batch != cache->batch || to->n_kv_heads != cache->n_kv_heads) return MINF_ERR_SHAPE;
   if (!places_differ(rows_of(to->k, to->k_stride, to->batch, to->n_kv_heads, to->capacity)) ||
       !places_differ(rows_of(to->v, to->v_stride, to->batch, to->n_kv_heads, to->capacity))) return MINF_ERR_SHAPE;
+  // K, V and weights of `to` in places of their own: they move at the same time
+  if (!input_apart(rows_of(to->k, to->k_stride, to->batch, to->n_kv_heads, to->capacity),
+                   rows_of(to->v, to->v_stride, to->batch, to->n_kv_heads, to->capacity)) ||
+      weight_range(to).meets(k_range(to)) || weight_range(to).meets(v_range(to))) return MINF_ERR_SHAPE;
   if (n_init < 0 || n_recent < 0 || keep < 1 || (int64_t)n_init + n_recent > keep) return MINF_ERR_BUDGET;
   const bool in_place = to->k == cache->k;
   if (in_place) {

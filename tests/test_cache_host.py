@@ -78,7 +78,8 @@ def test_cache_attn_refuses(L):
         assert attn(L, queries(**{name: None}), c) == NULL
     for kw in (dict(head_dim=64), dict(batch=0), dict(n_kv_heads=0), dict(capacity=0), dict(k=16 * GB + 8), dict(v=16 * GB + 2),
                dict(lens=16 * GB + 1), dict(k_stride=(1 << 20, 1 << 18, 64)), dict(v_stride=(1 << 20, 1 << 18, 132)),
-               dict(k_stride=(1 << 20, 1 << 18, (1 << 24) + 8)), dict(k_stride=(-8, 1 << 18, 128)), dict(n_kv_heads=3)):
+               dict(k_stride=(1 << 20, 1 << 18, (1 << 24) + 8)), dict(k_stride=(-8, 1 << 18, 128)), dict(n_kv_heads=3),
+               dict(capacity=(1 << 29) + 1)):
         assert attn(L, x, cache(**kw)) == SHAPE, kw
     for kw in (dict(n_q_heads=0), dict(n_q_heads=3), dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")),
                dict(softmax_scale=float("inf")), dict(q=GB + 8), dict(o=2 * GB + 2), dict(q_stride=(512, 128, 4)),
@@ -101,6 +102,12 @@ def test_outputs_must_not_lie_over_inputs(L):
     assert attn(L, queries(q=16 * GB, o=16 * GB, q_stride=(1000 * 1024, 128, 1024), o_stride=(1000 * 1024, 128, 1024)), fused) == WORKSPACE
     assert attn(L, queries(o=c.weight), c) == WORKSPACE                 # not written, not read
     assert attn(L, queries(o=c.weight), c, weights=1) == SHAPE
+    # weights of more than 16 rows per K/V head are computed from q when o is there already
+    assert attn(L, queries(32, o=x.q), cache(), weights=1) == WORKSPACE
+    assert attn(L, queries(34, o=x.q), cache(), weights=1) == SHAPE
+    assert attn(L, queries(34, o=x.q), cache()) == WORKSPACE
+    for where in (c.k, c.v + 256, x.q, c.lens):
+        assert attn(L, x, cache(weight=where), weights=1) == SHAPE and attn(L, x, cache(weight=where)) == WORKSPACE
     for stride in ((0, 1000), (2000, 999), (1000, 1000), (2000, 0)):
         assert attn(L, x, cache(weight_stride=stride), weights=2) == SHAPE, stride
     assert attn(L, x, cache(weight_stride=(1000, 2000)), weights=2) == WORKSPACE
@@ -144,6 +151,12 @@ def test_cache_evict_refuses(L):
     for kept in (c.k, c.weight, c.lens, c.v + 512, 4 * GB + 2):
         assert run(kept=ctypes.c_void_p(kept)) == SHAPE
     assert run(to=other(), kept=ctypes.c_void_p(32 * GB)) == SHAPE
+    # K and V move at the same time
+    both = cache(v=c.k)
+    assert run(c=both) == SHAPE and run(c=both, to=other()) == WORKSPACE and run(to=other(v=32 * GB)) == SHAPE
+    assert run(to=other(weight=32 * GB)) == SHAPE
+    fused = cache(k=16 * GB, v=16 * GB + 512, k_stride=(1000 * 512, 128, 512), v_stride=(1000 * 512, 128, 512))
+    assert run(c=fused) == WORKSPACE                                    # in place in a fused token-major buffer
     # broadcast caches can be read, not evicted in place
     flat = cache(k_stride=(0, 1000 * 128, 128))
     assert run(c=flat) == SHAPE and run(c=flat, to=other()) == WORKSPACE
