@@ -3,14 +3,17 @@
 //   o_i = sum_j p_ij v_j,  p_ij = exp(c q_i k_j - m_i) / sum_j' exp(c q_i k_j' - m_i),  j over the visible slots
 //   w_j (+)= sum over the rows i of a K/V head's group of p_ij
 //
-// Every key costs 512 bytes and, with R rows per K/V head, 512 R flops: with the 4 to 64 rows of a decode step
-// the memory bounds it, so the kernel is built to keep loads in flight.  A wave is a worker of its own: it
-// takes a consecutive share of the tiles of all sequences (cache_walk.h), fetches tile t+1 into its half of an
-// LDS ring (global -> LDS, no registers) while it computes tile t, and meets no barrier.  Rows are the columns
-// of 16x16x32 MFMAs (S^T = K Q^T, O^T += V^T P^T): the accumulator layout of S^T is the operand layout that the
-// second product needs, so P never leaves registers.
-// A segment (row tile of a sequence and K/V head) that several workers share leaves pieces (reference, sum,
-// unnormalised O) in the workspace, which cache_join_kernel joins.
+// Every key costs 512 bytes and, with R rows per K/V head, 512 R flops: up to some hundred rows the memory bounds
+// it, so the kernels are built to keep loads in flight.
+// Up to 32 rows (cache_attn_kernel): a wave is a worker of its own.  It takes a consecutive share of the tiles of
+// all sequences (cache_walk.h), fetches tile t+1 into its half of an LDS ring (global -> LDS, no registers) while it
+// computes tile t, and meets no barrier.  Rows are the columns of 16x16x32 MFMAs (S^T = K Q^T, O^T += V^T P^T): the
+// accumulator layout of S^T is the operand layout that the second product needs, so P never leaves registers.
+// (8 heads of 4 rows, 128K keys: 537 MB of K and V, the call 103 us, 5.2 TB/s.)
+// More rows (cache_shared_kernel, and cache_prefix_kernel for a prefix of more than 128): the waves of a workgroup
+// share the tiles.
+// A segment (row tile of a sequence and K/V head) that several workers or workgroups share leaves pieces
+// (reference, sum, unnormalised O) in the workspace, which cache_join_kernel joins.
 #include <type_traits>
 
 #include "cache_walk.h"
@@ -252,9 +255,11 @@ __device__ inline bool tile_not_finite(const char *tV, int lane) {
   return __builtin_amdgcn_ballot_w64(bad) != 0;
 }
 
-// Logits on their way to memory (for the weights).  They wait in LDS, as they lie in memory, [tile][row][32], and
-// go out 1 KiB a store: the loop counts its loads down in order, and every store it waits for on the way costs it
-// (tiles stored one by one: 1M tokens, 8 heads of 4 rows, 963 us; without the stores 717).
+// Logits on their way to memory (for the weights).  They are collected in LDS, as they lie in memory, [tile][row][32],
+// and go out in one burst of up to 8 KiB: memory that is read at full rate pays for writes in between by more than
+// their bytes, and for small ones most.  (8 heads of 4 rows, 1M tokens, 4.3 GB read and 134 MB written: tiles stored
+// one by one 963 us, in bursts 910, without the stores 717.  A loop that only reads and stores as much: 702 without
+// stores, 960 with 1 KiB a tile, 855 with 8 KiB every 16 tiles, 813 with 32 KiB, for which LDS has no room.)
 struct CacheLogits {
   char *room;            // CACHE_LOGITS bytes of LDS
   char *to;              // of the part's next tile in memory
@@ -853,9 +858,9 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void 
 }
 
 // ---- joining the pieces ---------------------------------------------------------------------------------
-// o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the pieces of the row's
-// own segment, of the prefix's and of the common slots.  Four waves share a row (W = 4: every fourth piece each) or, of
-// many rows, each wave takes one (W = 1); eight pieces at a time with all their loads in flight.  Rows without a visible key, or without a token, give zeros.
+// o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the pieces of the row's own segment and of the prefix's.
+// Four waves share a row (W = 4: every fourth piece each) or, of many rows, each wave takes one (W = 1); eight pieces at
+// a time with all their loads in flight.  Rows without a visible key, or without a token, give zeros.
 // Further workgroups give the slots their weights (where the logits were kept): they need the references and sums
 // of a K/V head's rows, which they join themselves, rather than wait for another launch.
 constexpr int JOIN_WAVES = 4, JOIN_AHEAD = 8;

@@ -166,6 +166,80 @@ def test_a_hidden_value_between_the_rows_windows(B):
     assert torch.equal(o[:, :, 1:], want[:, :, 1:])
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -3.3895313892515355e38])
+@pytest.mark.parametrize("T", [5, 16, 33])
+def test_hidden_slots_do_not_matter_to_many_rows(B, bad, T):
+    """The same of 20, 64 and 132 rows per K/V head, with and without the weights."""
+    cap, n, n_init, n_local = 1400, 1300, 70, 333
+    cache = cache_of(B, 40, 1, 2, cap, [n], fill=bad)
+    for t in (cache.k, cache.v):
+        t[:, :, n_init:n - T - n_local + 1] = bad            # no row sees these
+        t[:, :, n - 1] = bad                                 # only the last row does
+    q = queries(40, 1, 8, T)
+    clean = cache_of(B, 40, 1, 2, cap, [n])
+    rows = B.KVCache(clean.k, clean.v, torch.tensor([n - 1], dtype=torch.int32, device="cuda"))
+    for weights in (None, "set"):
+        o = attend(B, q, cache, n_init, n_local, weights=weights)
+        check_attention(q[:, :, :T - 1], rows, o[:, :, :T - 1], n_init, n_local)
+    assert (cache.weight[0, :, n_init:n - T - n_local + 1] == 0).all()
+
+
+@pytest.mark.parametrize("T", [5, 12, 33])
+def test_a_hidden_value_between_the_windows_of_many_rows(B, T):
+    """A slot that the first token still sees and the later ones do not (20, 48 and 132 rows)."""
+    n, n_local = 500, 150
+    cache = cache_of(B, 41, 1, 1, 512, [n])
+    first = n - T - n_local + 1
+    cache.v[:, :, first] = float("nan")
+    q = queries(41, 1, 4, T)
+    o = attend(B, q, cache, 0, n_local)
+    assert torch.isnan(o[:, :, 0].float()).all()
+    cache.v[:, :, first] = 0.0
+    want = attend(B, q, cache, 0, n_local)
+    assert torch.equal(o[:, :, 1:], want[:, :, 1:])
+
+
+@pytest.mark.parametrize("mode", [None, "set", "add"])
+@pytest.mark.parametrize("case", [(2, 8, 2, 5, 900, [900, 4], 30, 200), (1, 28, 4, 4, 3100, [3099], 0, BIG), (3, 17, 1, 1, 70, [70, 1, 33], 2, 9)],
+                         ids=["20", "28", "17"])
+def test_two_blocks_of_rows(B, case, mode):
+    """17 to 32 rows per K/V head."""
+    batch, hq, hkv, T, cap, lens, n_init, n_local = case
+    cache = cache_of(B, 42, batch, hkv, cap, lens)
+    q = queries(42, batch, hq, T)
+    if mode is not None:
+        for b, n in enumerate(lens):
+            cache.weight[b, :, :n] = 0.0
+    before = cache.weight.clone()
+    o = attend(B, q, cache, n_init, n_local, weights=mode)
+    check_attention(q, cache, o, n_init, n_local, before=before if mode else None)
+    assert mode or torch.equal(cache.weight, before)
+
+
+def test_output_in_place_of_many_query_rows(B):
+    """o = q with 128 rows and several workgroups a row; with weights, which need q once more, it is refused."""
+    cache = cache_of(B, 43, 1, 2, 9000, [8990])
+    q = queries(43, 1, 8, 32)
+    want = attend(B, q, cache)
+    with pytest.raises(B.MinfError):
+        attend(B, q, cache, weights="set", o=q)
+    assert torch.equal(attend(B, q, cache).view(torch.int16), want.view(torch.int16))
+    attend(B, q, cache, o=q)
+    assert torch.equal(q.view(torch.int16), want.view(torch.int16))
+
+
+def test_hidden_values_behind_a_prefix(B):
+    """NaN behind the prefix's length and the sequences', few and many rows."""
+    for batch, hq in ((2, 4), (10, 8), (40, 8)):
+        cache = cache_of(B, 44, batch, 2, 100, [1 + i for i in range(batch)])
+        prefix = cache_of(B, 45, 1, 2, 900, [795], weight=False)
+        q = queries(44, batch, hq, 1)
+        o = torch.full_like(q, float("nan"))
+        B.minf_prefix_attn(q, o, prefix, cache, workspace(B.minf_prefix_attn_workspace_bytes(q, prefix, cache)))
+        torch.cuda.synchronize()
+        check_attention(q, cache, o, prefix=prefix)
+
+
 def test_large_and_negative_logits(B):
     """Logits of some hundreds: the running maximum carries the sums."""
     cache = cache_of(B, 6, 1, 1, 1500, [1500])
