@@ -1350,13 +1350,32 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_select_kernel(EvictCall 
 
 // Long rows: a row in chunks, a workgroup each.  Pass p counts its digit per chunk; the workgroups of the next
 // launch each add up the row's counts and pick the digit themselves (no atomics on memory, nothing to clear).
+// The row and chunk of a workgroup.  Workgroups go round the eight XCDs: a row's are put on as few of them as keep
+// all busy, since they read each other's counts, through the XCD's L2.
+struct SelectPlace {
+  int row, chunk;
+  __device__ inline explicit SelectPlace(const EvictCall &x) {
+    const int rows = x.batch * x.n_kv, id = blockIdx.x, xcd = id & 7, turn = id >> 3;
+    if (rows % 8 == 0) {
+      row = turn / x.chunks * 8 + xcd;
+      chunk = turn % x.chunks;
+    } else if (8 % rows == 0) {
+      row = xcd % rows;
+      chunk = turn * (8 / rows) + xcd / rows;
+    } else {
+      row = id / x.chunks;
+      chunk = id % x.chunks;
+    }
+  }
+};
+
 template <int PASS>
 __device__ inline void select_from_counts(const EvictCall &x, int row, int chunk, unsigned &key, int &want, int &gt, int &eq,
                                           SelectLds &s) {
   const int hi = select_bins(PASS) - 1 - 2 * (int)threadIdx.x;
   int n[2] = {0, 0}, before[2] = {0, 0};
   if (hi > 0) {
-    const unsigned *h = x.hist + (((int64_t)PASS * gridDim.y + row) * x.chunks * SELECT_BINS + (hi - 1)) / 2;
+    const unsigned *h = x.hist + (((int64_t)PASS * x.batch * x.n_kv + row) * x.chunks * SELECT_BINS + (hi - 1)) / 2;
 #pragma unroll 8
     for (int c = 0; c < x.chunks; ++c) {
       const unsigned two = h[(int64_t)c * (SELECT_BINS / 2)];
@@ -1374,7 +1393,9 @@ __device__ inline void select_from_counts(const EvictCall &x, int row, int chunk
 template <int PASS>
 __global__ __launch_bounds__(SELECT_THREADS) void cache_count_kernel(EvictCall x) {
   __shared__ SelectLds s;
-  const int chunk = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  const SelectPlace at(x);
+  const int row = at.row, chunk = at.chunk, tid = threadIdx.x;
+  if (chunk >= x.chunks) return;
   const SelectRow r(x, row);
   const int from = chunk * x.chunk_slots, to = min(from + x.chunk_slots, r.len);
   if (r.len <= x.keep || r.want == 0) return;
@@ -1390,7 +1411,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_count_kernel(EvictCall x
     if (tid == 0) *state = SelectState{key, want, gt};
   }
   select_count<PASS>(keys, key, s);
-  unsigned *h = x.hist + (((int64_t)PASS * gridDim.y + row) * x.chunks + chunk) * (SELECT_BINS / 2);
+  unsigned *h = x.hist + (((int64_t)PASS * x.batch * x.n_kv + row) * x.chunks + chunk) * (SELECT_BINS / 2);
   for (int i = tid; i < select_bins(PASS) / 2; i += SELECT_THREADS) {
     int a = 0, b = 0;
 #pragma unroll
@@ -1401,7 +1422,9 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_count_kernel(EvictCall x
 
 __global__ __launch_bounds__(SELECT_THREADS) void cache_emit_kernel(EvictCall x) {
   __shared__ SelectLds s;
-  const int chunk = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  const SelectPlace at(x);
+  const int row = at.row, chunk = at.chunk, tid = threadIdx.x;
+  if (chunk >= x.chunks) return;
   const SelectRow r(x, row);
   int32_t *kept = x.kept + (int64_t)row * x.keep;
   if (chunk == 0 && tid == 0) x.counts[row] = min(r.len, x.keep);
@@ -1540,7 +1563,8 @@ hipError_t launch_cache_evict(const EvictCall &x, bool in_place, hipStream_t st)
   if (x.chunks == 0) {
     hipLaunchKernelGGL(cache_select_kernel, dim3(rows), dim3(SELECT_THREADS), 0, st, x);
   } else {
-    const dim3 grid(x.chunks, rows);
+    const int groups = rows % 8 != 0 && 8 % rows == 0 ? (x.chunks * rows + 7) / 8 * 8 : x.chunks * rows;
+    const dim3 grid(groups);
     hipLaunchKernelGGL(cache_count_kernel<0>, grid, dim3(SELECT_THREADS), 0, st, x);
     hipLaunchKernelGGL(cache_count_kernel<1>, grid, dim3(SELECT_THREADS), 0, st, x);
     hipLaunchKernelGGL(cache_count_kernel<2>, grid, dim3(SELECT_THREADS), 0, st, x);
