@@ -1146,9 +1146,9 @@ __global__ __launch_bounds__(256, 3) void cache_column_kernel(CacheCall x) {
 }
 
 // ---- eviction ---------------------------------------------------------------------------------------------
-// Order of the weights as unsigned numbers: NaN lowest, -0 and 0 equal.
+// Order of the weights as unsigned numbers: NaN lowest, -0 and 0 equal.  0 is no weight's.
 __device__ inline unsigned weight_key(float v) {
-  if (v != v) return 0u;
+  if (v != v) return 1u;
   const unsigned u = v == 0.f ? 0u : __builtin_bit_cast(unsigned, v);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -1202,15 +1202,12 @@ struct SelectLds {
 struct SelectKeys {
   static constexpr int BATCHES = 32768 / SELECT_THREADS / SELECT_AHEAD;
   unsigned k[BATCHES][SELECT_AHEAD];
-  int w0, w1;                      // this wave's slots, those that are chosen by weight among them: in(i)
-  int first;
+  int w0, w1;                      // this wave's slots; 0: not to be chosen by weight
   __device__ inline int slot(int t, int j, int lane) const { return w0 + 64 * (t * SELECT_AHEAD + j) + lane; }
   __device__ inline bool batch(int t) const { return w0 + 64 * SELECT_AHEAD * t < w1; }
-  __device__ inline bool in(int i) const { return i >= first && i < w1; }
   __device__ inline void load(const SelectRow &r, int from, int to) {
     const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
     const int per = (to - from + SELECT_THREADS - 1) / SELECT_THREADS * 64;
-    first = r.first;
     w0 = from + wave * per;
     w1 = min(w0 + per, min(to, r.last));
 #pragma unroll
@@ -1220,7 +1217,10 @@ struct SelectKeys {
 #pragma unroll
       for (int j = 0; j < SELECT_AHEAD; ++j) v[j] = r.w[min(slot(t, j, lane), w1 - 1)];
 #pragma unroll
-      for (int j = 0; j < SELECT_AHEAD; ++j) k[t][j] = weight_key(v[j]);
+      for (int j = 0; j < SELECT_AHEAD; ++j) {
+        const int i = slot(t, j, lane);
+        k[t][j] = i >= r.first && i < w1 ? weight_key(v[j]) : 0u;
+      }
     }
   }
 };
@@ -1229,7 +1229,7 @@ struct SelectKeys {
 // copies: weights cluster, and lanes that meet in a bin go one after the other.
 template <int PASS>
 __device__ inline void select_count(const SelectKeys &keys, unsigned prefix, SelectLds &s) {
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x;
   for (int i = tid; i < SELECT_COPIES * SELECT_BINS; i += SELECT_THREADS) (&s.hist[0][0])[i] = 0;
   __syncthreads();
 #pragma unroll
@@ -1238,7 +1238,7 @@ __device__ inline void select_count(const SelectKeys &keys, unsigned prefix, Sel
 #pragma unroll
     for (int j = 0; j < SELECT_AHEAD; ++j) {
       const unsigned k = keys.k[t][j];
-      if (keys.in(keys.slot(t, j, lane)) && (k & select_mask(PASS)) == prefix)
+      if (k != 0u && (k & select_mask(PASS)) == prefix)
         atomicAdd(&s.hist[tid & (SELECT_COPIES - 1)][(k >> select_shift(PASS)) & (select_bins(PASS) - 1)], 1);
     }
   }
@@ -1281,27 +1281,24 @@ __device__ inline void select_emit(const SelectRow &r, const SelectKeys &keys, i
     if (!keys.batch(t)) break;
 #pragma unroll
     for (int j = 0; j < SELECT_AHEAD; ++j) {
-      const bool here = keys.in(keys.slot(t, j, lane));
-      ng += __popcll(__builtin_amdgcn_ballot_w64(here && keys.k[t][j] > key));
-      ne += __popcll(__builtin_amdgcn_ballot_w64(here && keys.k[t][j] == key));
+      ng += keys.k[t][j] > key;
+      ne += keys.k[t][j] == key;
     }
   }
   int all;
-  const int before_g = block_scan(lane == 0 ? ng : 0, s.part, all), before_e = block_scan(lane == 0 ? ne : 0, s.part, all);
-  gt += uni(before_g);
+  const int before_g = block_scan(ng, s.part, all), before_e = block_scan(ne, s.part, all);
+  gt += uni(before_g);                                             // (the first lane's: those of the waves before)
   eq += uni(before_e);
 #pragma unroll
   for (int t = 0; t < SelectKeys::BATCHES; ++t) {
     if (!keys.batch(t)) break;
 #pragma unroll
     for (int j = 0; j < SELECT_AHEAD; ++j) {
-      const int i = keys.slot(t, j, lane);
-      const bool here = keys.in(i);
-      const unsigned long long g = __builtin_amdgcn_ballot_w64(here && keys.k[t][j] > key);
-      const unsigned long long e = __builtin_amdgcn_ballot_w64(here && keys.k[t][j] == key);
+      const unsigned k = keys.k[t][j];
+      const unsigned long long g = __builtin_amdgcn_ballot_w64(k > key), e = __builtin_amdgcn_ballot_w64(k == key);
       if ((g | e) == 0) continue;
       const int gr = rank(g, gt), er = rank(e, eq);
-      if ((here && keys.k[t][j] > key) || (here && keys.k[t][j] == key && er < want)) kept[r.first + gr + min(er, want)] = i;
+      if (k > key || (k == key && er < want)) kept[r.first + gr + min(er, want)] = keys.slot(t, j, lane);
       gt += __popcll(g);
       eq += __popcll(e);
     }
