@@ -530,6 +530,13 @@ struct CacheSource {
                  "global_load_lds_dwordx4 %5, %1 offset:3072"
                  :: "v"(ofs[0]), "s"(row0), "s"(lds), "v"(ofs[1]), "v"(ofs[2]), "v"(ofs[3]) : "memory");
   }
+  // 8 rows, the first or the second ones of 16 (their offsets: two of the four; row0, lds: of the 16, plus 2048 for the second)
+  __device__ static inline void rows8(const char *row0, unsigned ofs0, unsigned ofs1, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %0, %1\n\t"
+                 "global_load_lds_dwordx4 %3, %1 offset:1024"
+                 :: "v"(ofs0), "s"(row0), "s"(lds), "v"(ofs1) : "memory");
+  }
   // 32 rows from kb on into the tile at lds
   __device__ static inline void tile(const char *h, unsigned rb, const unsigned (&ofs)[4], int kb, unsigned lds) {
 #pragma unroll
@@ -672,20 +679,26 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
 }
 
 // ---- more than 32 rows -----------------------------------------------------------------------------------
-// Four waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile) and take 16 NB rows
-// each: 64 or 128 rows a workgroup.  Memory bounds it: 32 KiB a tile take a CU 1.4 us, about as long as the arithmetic of
-// 128 rows.  (128 rows, 8 heads of 128K tokens: 112 us; eight waves of 16 rows, which read every operand from LDS
-// twice as often, 132; the 256-row loop of cache_prefix_kernel 142.)  P in one bf16, as in the prefill kernels: the
-// matrix cores have no time to spare for its rest.
+// Eight waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile): four take the
+// first 32 keys and four the others, 16 NB rows each, 64 or 128 rows a workgroup; at the end the two halves' sums are
+// joined in LDS.  So a SIMD has two waves, one's exponentials beside the other's products, and no operand is read from
+// LDS more often than with four.  Memory bounds 128 rows (32 KiB a tile take a CU 1.4 us), the arithmetic more of them.
+// (128 rows, 8 heads of 128K tokens, and 256 rows, 4 heads of 40K: 110 and 39 us; four waves with all 64 keys 120 and
+// 44; two workgroups of four waves and 32-key tiles a CU 109 and 39, but twice the pieces to join, 3 us more; eight
+// waves of 16 rows, which read every operand twice as often, 132 us for the 128 rows; the 256-row loop of
+// cache_prefix_kernel 142.)  P in one bf16, as in the prefill kernels: off by 2^-8 of a probability at most, which is what
+// O itself is rounded by, and the errors of many keys cancel in part; its rest would take the matrix cores as long again
+// as the product with V.
 // A workgroup takes one part (of x.*_sh.splits) of the tiles that its rows see; a segment in one part is final, of
 // others reference, sum and unnormalised O go to the workspace for cache_join_kernel.
 // Launch order: the row tiles that read the same slots run on one XCD, one after the other.
-constexpr int SHARED_RING = 4 * 2 * TILE_BYTES, SHARED_ROOM = 4096;        // ROOM (per wave): update_by_token
+constexpr int SHARED_WAVES = 8, SHARED_RING = 4 * 2 * TILE_BYTES, SHARED_ROOM = 4096;    // ROOM (per wave): update_by_token
 template <int NB, bool PREFIX>
-__global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void cache_shared_kernel(CacheCall x) {
-  constexpr int W = CACHE_WAVES, prefix = PREFIX;
+__global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(CacheCall x) {
+  constexpr int W = SHARED_WAVES / 2, prefix = PREFIX;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = to_sgpr(threadIdx.x >> 6);
+  const int half = to_sgpr(wave / W), row_wave = wave - half * W;            // of a tile's keys; of the rows
   const SharedPart &sh = prefix ? x.p_sh : x.own_sh;
   const int splits = sh.splits, tile_rows = 16 * NB * W;
   const int per_xcd = blockIdx.x >> 3, turn = to_sgpr(per_xcd / sh.row_tiles), rt = per_xcd - turn * sh.row_tiles;
@@ -697,7 +710,7 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void 
   c.prefix = prefix;
   c.b = prefix ? 0 : to_sgpr(head / x.n_kv);
   c.kvh = head - c.b * x.n_kv;
-  c.rt = rt * W + wave;                                                      // row tile of 16 NB rows
+  c.rt = rt * W + row_wave;                                                  // row tile of 16 NB rows
   const int last_row = min((rt + 1) * tile_rows, sh.rows) - 1;
   const int len = to_sgpr(prefix ? x.p_lens[0] : x.lens[c.b]);
   const TileWalk<SHARED_TILE> w = prefix ? tile_walk<SHARED_TILE>(len, x.p_cap, 1, 0, x.p_cap)
@@ -716,18 +729,20 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void 
   src.strides(x, prefix, lane);
   src.heads(x, c);
   const unsigned ring = uni(lds_addr_of(lds));
-  constexpr int ROWS = 64 / W;                                               // of a tile, fetched by a wave
-  auto fetch = [&](int i) {
+  const int upper = wave & 1;
+  const unsigned k0 = upper ? src.kofs[2] : src.kofs[0], k1 = upper ? src.kofs[3] : src.kofs[1];
+  const unsigned v0 = upper ? src.vofs[2] : src.vofs[0], v1 = upper ? src.vofs[3] : src.vofs[1];
+  auto fetch = [&](int i) {                                                  // a wave: 8 rows of K and of V
     const unsigned to = ring + (i & 3) * (2 * TILE_BYTES);
     const int kb = w.base(t0 + min(i, n - 1)), end = kb + SHARED_TILE;
     if (end <= w.len && (kb >= w.lo || end <= w.e1)) {
-      const int row = kb + ROWS * wave;
-      const unsigned at = to_sgpr(to + 4096 * wave);
-      src.rows16(src.kh + (uint64_t)(unsigned)row * src.k_rb, src.kofs, at);
-      src.rows16(src.vh + (uint64_t)(unsigned)row * src.v_rb, src.vofs, at + TILE_BYTES);
+      const int row = kb + 16 * (wave >> 1);
+      const unsigned at = to_sgpr(to + 2048 * wave);
+      src.rows8(src.kh + (uint64_t)(unsigned)row * src.k_rb + 2048 * upper, k0, k1, at);
+      src.rows8(src.vh + (uint64_t)(unsigned)row * src.v_rb + 2048 * upper, v0, v1, at + TILE_BYTES);
     } else {
-      src.template rows_in_part<ROWS / 4>(src.kh, src.k_rb, kb, ROWS * wave, w, to, lane);
-      src.template rows_in_part<ROWS / 4>(src.vh, src.v_rb, kb, ROWS * wave, w, to + TILE_BYTES, lane);
+      src.template rows_in_part<2>(src.kh, src.k_rb, kb, 8 * wave, w, to, lane);
+      src.template rows_in_part<2>(src.vh, src.v_rb, kb, 8 * wave, w, to + TILE_BYTES, lane);
     }
   };
   CacheRows<NB> st;
@@ -756,14 +771,14 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void 
   lo.init(lane);
   const float c_log2 = x.c_log2;
   for (int i = 0; i < n; ++i) {
-    MINF_WAIT_VMCNT(16);                       // this wave's part of tile i; those of i + 1 and i + 2 may run
+    MINF_WAIT_VMCNT(8);                        // this wave's part of tile i; those of i + 1 and i + 2 may run
     __syncthreads();                           // all of tile i is there; all waves are done with tile i - 1
     fetch(i + 3);                              // behind the last tile it is repeated: every tile issues as many loads
-    const char *tK = lds + (i & 3) * (2 * TILE_BYTES), *tV = tK + TILE_BYTES;
-    const int kb = w.base(t0 + i);
-    f32x4 s[4][NB];                            // [16 keys][row block]
+    const char *tK = lds + (i & 3) * (2 * TILE_BYTES) + half * HALF_BYTES, *tV = tK + TILE_BYTES;
+    const int kb = w.base(t0 + i) + CACHE_TILE * half;
+    f32x4 s[2][NB];                            // [16 keys][row block]
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
         const bf16x8 a = lds_read_k(tK, lo.k[ks] + kt * HALF_TILE_ROWS);
@@ -773,12 +788,12 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void 
           s[kt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, st.q.q[nb][ks], ks == 0 ? zero : s[kt][nb], 0, 0, 0);
         }
       }
-    const bool edge = !mask.whole<SHARED_TILE>(kb);
+    const bool edge = !mask.whole<CACHE_TILE>(kb);
     if (edge) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
+        for (int e = 0; e < 8; ++e)
           s[e >> 2][nb][e & 3] = cache_visible(kb + 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3), st.pos[nb], mask.n_init, mask.n_local)
                                      ? s[e >> 2][nb][e & 3] : -INFINITY;
     }
@@ -788,7 +803,7 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void 
     for (int nb = 0; nb < NB; ++nb) {
       mx[nb] = s[0][nb][0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) mx[nb] = fmaxf(mx[nb], s[e >> 2][nb][e & 3]);
+      for (int e = 1; e < 8; ++e) mx[nb] = fmaxf(mx[nb], s[e >> 2][nb][e & 3]);
       outgrown = outgrown || mx[nb] * c_log2 > st.m[nb] + REF_ROOM;
     }
     if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
@@ -804,33 +819,28 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void 
         for (int db = 0; db < 8; ++db) st.o[nb][db] *= f;
       }
     }
-    const bool by_token = !PREFIX && edge && mask.n_tok > 1 && tile_not_finite<TILE_BYTES>(tV, lane);
+    bf16x8 p[NB][1];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      bf16x8 p[NB][1];
+    for (int nb = 0; nb < NB; ++nb) {
+      const float m = st.m[nb] == -INFINITY ? 0.f : st.m[nb];
+      float sum = 0.f;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const float m = st.m[nb] == -INFINITY ? 0.f : st.m[nb];
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          const f32x4 &v4 = s[2 * half + (e >> 2)][nb];
-          const f32x2 v = {fast_exp2(fmaf(v4[e & 3], c_log2, -m)), fast_exp2(fmaf(v4[(e & 3) + 1], c_log2, -m))};
-          sum += v[0] + v[1];
-          const bf16x2 two = __builtin_convertvector(v, bf16x2);
-          p[nb][0][e] = two[0];
-          p[nb][0][e + 1] = two[1];
-        }
-        st.l[nb] += sum;
+      for (int e = 0; e < 8; e += 2) {
+        const f32x4 &v4 = s[e >> 2][nb];
+        const f32x2 v = {fast_exp2(fmaf(v4[e & 3], c_log2, -m)), fast_exp2(fmaf(v4[(e & 3) + 1], c_log2, -m))};
+        sum += v[0] + v[1];
+        const bf16x2 two = __builtin_convertvector(v, bf16x2);
+        p[nb][0][e] = two[0];
+        p[nb][0][e + 1] = two[1];
       }
-      if (by_token) {
-        update_by_token<NB, 1>(st, p, tV + half * HALF_BYTES, lds + SHARED_RING + wave * SHARED_ROOM, kb + CACHE_TILE * half, mask, lane);
-        continue;
-      }
+      st.l[nb] += sum;
+    }
+    if (!PREFIX && edge && mask.n_tok > 1 && tile_not_finite<HALF_BYTES>(tV, lane)) {
+      update_by_token<NB, 1>(st, p, tV, lds + SHARED_RING + wave * SHARED_ROOM, kb, mask, lane);
+    } else {
 #pragma unroll
       for (int db = 0; db < 8; ++db) {
-        const int at = lo.v[db] + half * HALF_BYTES;
-        const bf16x8 a = lds_read_vt(tV, at, at + HALF_TILE_ROWS);
+        const bf16x8 a = lds_read_vt(tV, lo.v[db], lo.v[db] + HALF_TILE_ROWS);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][0], st.o[nb][db], 0, 0, 0);
       }
@@ -838,10 +848,35 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 2 && !PREFIX ? 1 : 2) void 
     __builtin_amdgcn_s_waitcnt(0xC07F);        // LDS reads done
   }
   MINF_WAIT_VMCNT(0);                          // the repeated loads
+  // The two halves' sums, in the place of the ring: the same lane has the same row and the same d of both.
+  __syncthreads();
+  f32x4 *other_o = reinterpret_cast<f32x4 *>(lds) + row_wave * (NB * 8 * 64) + lane;
+  float2 *other_ml = reinterpret_cast<float2 *>(lds + W * NB * 8 * 64 * 16) + row_wave * (NB * 64) + lane;
+  if (half == 1) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      other_ml[64 * nb] = float2{st.m[nb], st.l[nb]};
+#pragma unroll
+      for (int db = 0; db < 8; ++db) other_o[64 * (8 * nb + db)] = st.o[nb][db];
+    }
+  }
+  __syncthreads();
+  if (half == 1) return;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const float2 ml = other_ml[64 * nb];
+    const float m = fmaxf(st.m[nb], ml.x);
+    // (-inf: no key was seen, the sums are 0)
+    const float f0 = st.m[nb] == -INFINITY ? 1.f : fast_exp2(st.m[nb] - m), f1 = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - m);
+    st.m[nb] = m;
+    st.l[nb] = st.l[nb] * f0 + ml.y * f1;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) st.o[nb][db] = st.o[nb][db] * f0 + other_o[64 * (8 * nb + db)] * f1;
+  }
   const int64_t item = ((int64_t)head * sh.row_tiles + rt) * splits + part;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const int in_tile = (wave * NB + nb) * 16 + (lane & 15), row = rt * tile_rows + in_tile;
+    const int in_tile = (row_wave * NB + nb) * 16 + (lane & 15), row = rt * tile_rows + in_tile;
     float l = st.l[nb] + __shfl_xor(st.l[nb], 16);
     l += __shfl_xor(l, 32);
     if (row >= sh.rows) continue;
@@ -1518,12 +1553,12 @@ static hipError_t launch_workers(const CacheCall &x, hipStream_t st) {
 
 template <int NB, bool PREFIX>
 static hipError_t launch_shared_as(const CacheCall &x, const SharedPart &sh, hipStream_t st) {
-  const size_t lds = SHARED_RING + CACHE_WAVES * SHARED_ROOM;
+  const size_t lds = SHARED_RING + SHARED_WAVES * SHARED_ROOM;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_shared_kernel<NB, PREFIX>),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
   const int groups = (PREFIX ? 1 : x.batch) * x.n_kv * sh.splits;
-  hipLaunchKernelGGL((cache_shared_kernel<NB, PREFIX>), dim3((groups + 7) / 8 * 8 * sh.row_tiles), dim3(64 * CACHE_WAVES), lds, st, x);
+  hipLaunchKernelGGL((cache_shared_kernel<NB, PREFIX>), dim3((groups + 7) / 8 * 8 * sh.row_tiles), dim3(64 * SHARED_WAVES), lds, st, x);
   return hipGetLastError();
 }
 template <bool PREFIX>

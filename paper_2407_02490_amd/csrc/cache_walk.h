@@ -122,7 +122,7 @@ MINF_HD int32_t piece_slot(int32_t worker, int32_t t0, int32_t share) {
   return 2 * worker + (t0 > worker * share ? 1 : 0);
 }
 
-// Tiles that four waves take together are cut into at most `splits` parts of equally many: tiles per part.
+// Tiles that the waves of a workgroup take together are cut into at most `splits` parts of equally many: tiles per part.
 MINF_HD int32_t part_tiles(int32_t tiles, int32_t splits) { return (tiles + splits - 1) / splits; }
 MINF_HD int32_t part_count(int32_t tiles, int32_t splits) {
   const int32_t per = part_tiles(tiles, splits);

@@ -221,7 +221,7 @@ hipError_t launch_build_bs(const QKV &x, int nb, const HeadList &hl, int topk, i
 
 // ---- the cache calls (cache_kernels.hip) --------------------------------------------------------------------
 // Pointers of device memory, strides in elements (_sb: sequence, _sh: head, _st: token).
-// Rows that four waves take together, tile_rows at a time, their tiles cut into `splits` parts: 64 or 128 of them
+// Rows that the waves of a workgroup take together, tile_rows at a time, their tiles cut into `splits` parts: 64 or 128 of them
 // cache_shared_kernel, 256 cache_prefix_kernel (of a prefix, its whole tiles of 64; the rest is the workers').
 struct SharedPart {
   int32_t on, rows, tile_rows, row_tiles, splits;
