@@ -179,6 +179,7 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
     p.need = p.at_logits;
     if (x.rows <= 16) p.need += up(heads * x.max_tiles * x.rows * CACHE_TILE * sizeof(float));
   }
+  if (p.need == 0) p.need = 256;                                       // 0 is the answer to invalid arguments
   return MINF_OK;
 }
 

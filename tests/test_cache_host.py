@@ -186,6 +186,14 @@ def test_workspace_sizes(L):
     assert L.minf_cache_attn_workspace_bytes(REF(queries(8)), REF(huge), 0, 1 << 12, 0) == 0
 
 
+def test_a_call_that_needs_no_memory_names_a_workspace_all_the_same(L):
+    """0 is the answer to invalid arguments, and a workspace without bytes has no address."""
+    x, c = queries(8, 16, q_stride=(1 << 14, 2048, 128), o_stride=(1 << 14, 2048, 128)), cache(2, 2, 40)      # 64 rows, one tile
+    n = L.minf_cache_attn_workspace_bytes(REF(x), REF(c), 0, 40, 0)
+    assert n > 0
+    assert attn(L, x, c, 0, 40, 0, None, n) == WORKSPACE and attn(L, x, c, 0, 40, 0, WS, n - 1) == WORKSPACE
+
+
 def test_binding_checks_its_tensors():
     import torch
     from paper_2407_02490_amd import binding as B

@@ -216,6 +216,22 @@ def test_two_blocks_of_rows(B, case, mode):
     assert mode or torch.equal(cache.weight, before)
 
 
+@pytest.mark.parametrize("mode", [None, "set", "add"])
+@pytest.mark.parametrize("case", [(3, 8, 2, 16, 50, [50, 15, 0], 0, BIG), (40, 16, 8, 40, 130, [130 - 3 * i for i in range(40)], 9, 60)],
+                         ids=["one-tile", "320-heads"])
+def test_segments_that_one_workgroup_takes_whole(B, case, mode):
+    """More than 32 rows without pieces: O is written at once."""
+    batch, hq, hkv, T, cap, lens, n_init, n_local = case
+    cache = cache_of(B, 46, batch, hkv, cap, lens)
+    q = queries(46, batch, hq, T)
+    if mode is not None:
+        for b, n in enumerate(lens):
+            cache.weight[b, :, :n] = 0.0
+    before = cache.weight.clone()
+    o = attend(B, q, cache, n_init, n_local, weights=mode)
+    check_attention(q, cache, o, n_init, n_local, before=before if mode else None)
+
+
 def test_output_in_place_of_many_query_rows(B):
     """o = q with 128 rows and several workgroups a row; with weights, which need q once more, it is refused."""
     cache = cache_of(B, 43, 1, 2, 9000, [8990])
