@@ -83,15 +83,20 @@ struct Plan {
 
 // How the rows of `heads` K/V heads (of a sequence) are taken, whole: 256 at a time: row tiles, and parts such that the
 // workgroups, one per CU, come in rounds of least time.  A workgroup's start and end cost as much as six tiles.
-void plan_shared(SharedPart &p, int64_t heads, int64_t rows, int64_t tiles, bool whole) {
+// ragged: the tiles are those of a full cache, of several sequences whose lengths the host does not know.  Then the time
+// counts as well that parts of any length, half of a full one on average, take when a CU that is done takes the next.
+void plan_shared(SharedPart &p, int64_t heads, int64_t rows, int64_t tiles, bool whole, bool ragged) {
   p.on = 1;
   p.rows = (int32_t)rows;
   p.tile_rows = rows <= 64 ? 64 : rows <= 128 || !whole ? 128 : 256;
   p.row_tiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
   p.splits = 1;
+  const int64_t segments = heads * p.row_tiles, cost = 6;
   int64_t least = INT64_MAX;
   for (int s = 1; s <= 64 && s <= tiles; ++s) {
-    const int64_t time = (heads * p.row_tiles * s + CUS - 1) / CUS * (part_tiles((int32_t)tiles, s) + 6);
+    const int64_t part = part_tiles((int32_t)tiles, s) + cost;
+    int64_t time = (segments * s + CUS - 1) / CUS * part;
+    if (ragged) time += segments * (tiles / 2 + cost * s) / CUS + part;
     if (time < least) { least = time; p.splits = s; }
   }
 }
@@ -139,7 +144,8 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   x.max_tiles = (int32_t)((seen + CACHE_TILE - 1) / CACHE_TILE);
   int64_t segments = (int64_t)x.batch * x.n_kv * x.row_tiles;
   int64_t places = segments * (x.max_tiles + SEGMENT_COST);
-  if (own_sh) plan_shared(x.own_sh, (int64_t)x.batch * x.n_kv, x.rows, (seen + SHARED_TILE - 1) / SHARED_TILE, false);
+  if (own_sh) plan_shared(x.own_sh, (int64_t)x.batch * x.n_kv, x.rows, (seen + SHARED_TILE - 1) / SHARED_TILE, false,
+                          x.batch > 1 && seen == x.capacity);
   if (prefix) {
     x.pk = static_cast<const bf16_t *>(prefix->k); x.pv = static_cast<const bf16_t *>(prefix->v);
     x.p_lens = prefix->lens;
@@ -148,7 +154,7 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
     x.p_cap = prefix->capacity;
     segments += (int64_t)x.n_kv * x.p_row_tiles;
     places += (int64_t)x.n_kv * x.p_row_tiles * ((prefix->capacity + CACHE_TILE - 1) / CACHE_TILE + SEGMENT_COST);
-    if (p_sh) plan_shared(x.p_sh, x.n_kv, p_rows, (prefix->capacity + SHARED_TILE - 1) / SHARED_TILE, true);
+    if (p_sh) plan_shared(x.p_sh, x.n_kv, p_rows, (prefix->capacity + SHARED_TILE - 1) / SHARED_TILE, true, false);
   }
   if (places >= (int64_t)1 << 30) return MINF_ERR_SHAPE;               // the list of tiles is counted in 32 bits
   x.workers = CUS * 4;

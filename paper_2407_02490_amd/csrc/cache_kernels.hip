@@ -686,16 +686,17 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
 // (128 rows, 8 heads of 128K tokens, and 256 rows, 4 heads of 40K: 110 and 39 us; four waves with all 64 keys 120 and
 // 44; two workgroups of four waves and 32-key tiles a CU 109 and 39, but twice the pieces to join, 3 us more; eight
 // waves of 16 rows, which read every operand twice as often, 132 us for the 128 rows; the 256-row loop of
-// cache_prefix_kernel 142.)  P in one bf16, as in the prefill kernels: off by 2^-8 of a probability at most, which is what
-// O itself is rounded by, and the errors of many keys cancel in part; its rest would take the matrix cores as long again
-// as the product with V.
+// cache_prefix_kernel 142.)
+// P in two bf16 up to 64 rows.  Beyond in one, as in the prefill kernels: off by 2^-8 of a probability at most, which is
+// what O itself is rounded by, and the errors of many keys cancel in part; its rest would take the matrix cores as long
+// again as the product with V.
 // A workgroup takes one part (of x.*_sh.splits) of the tiles that its rows see; a segment in one part is final, of
 // others reference, sum and unnormalised O go to the workspace for cache_join_kernel.
 // Launch order: the row tiles that read the same slots run on one XCD, one after the other.
 constexpr int SHARED_WAVES = 8, SHARED_RING = 4 * 2 * TILE_BYTES, SHARED_ROOM = 4096;    // ROOM (per wave): update_by_token
 template <int NB, bool PREFIX>
 __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(CacheCall x) {
-  constexpr int W = SHARED_WAVES / 2, prefix = PREFIX;
+  constexpr int W = SHARED_WAVES / 2, PARTS = NB == 1 ? 2 : 1, prefix = PREFIX;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = to_sgpr(threadIdx.x >> 6);
   const int half = to_sgpr(wave / W), row_wave = wave - half * W;            // of a tile's keys; of the rows
@@ -819,7 +820,7 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
         for (int db = 0; db < 8; ++db) st.o[nb][db] *= f;
       }
     }
-    bf16x8 p[NB][1];
+    bf16x8 p[NB][PARTS];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const float m = st.m[nb] == -INFINITY ? 0.f : st.m[nb];
@@ -827,22 +828,29 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         const f32x4 &v4 = s[e >> 2][nb];
-        const f32x2 v = {fast_exp2(fmaf(v4[e & 3], c_log2, -m)), fast_exp2(fmaf(v4[(e & 3) + 1], c_log2, -m))};
+        f32x2 v = {fast_exp2(fmaf(v4[e & 3], c_log2, -m)), fast_exp2(fmaf(v4[(e & 3) + 1], c_log2, -m))};
         sum += v[0] + v[1];
-        const bf16x2 two = __builtin_convertvector(v, bf16x2);
-        p[nb][0][e] = two[0];
-        p[nb][0][e + 1] = two[1];
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+          const bf16x2 two = __builtin_convertvector(v, bf16x2);
+          p[nb][part][e] = two[0];
+          p[nb][part][e + 1] = two[1];
+          v = f32x2{v[0] - (float)two[0], v[1] - (float)two[1]};
+        }
       }
       st.l[nb] += sum;
     }
     if (!PREFIX && edge && mask.n_tok > 1 && tile_not_finite<HALF_BYTES>(tV, lane)) {
-      update_by_token<NB, 1>(st, p, tV, lds + SHARED_RING + wave * SHARED_ROOM, kb, mask, lane);
+      update_by_token<NB, PARTS>(st, p, tV, lds + SHARED_RING + wave * SHARED_ROOM, kb, mask, lane);
     } else {
 #pragma unroll
       for (int db = 0; db < 8; ++db) {
         const bf16x8 a = lds_read_vt(tV, lo.v[db], lo.v[db] + HALF_TILE_ROWS);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][0], st.o[nb][db], 0, 0, 0);
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int part = 0; part < PARTS; ++part)
+            st.o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[nb][part], st.o[nb][db], 0, 0, 0);
       }
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);        // LDS reads done
