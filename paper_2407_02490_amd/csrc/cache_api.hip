@@ -129,8 +129,13 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   x.c_log2 = scale * 1.4426950408889634f;
   x.rows = x.group * x.n_new;
   const int64_t p_rows = prefix ? (int64_t)x.batch * x.rows : 0;
-  // rows that the workers take: up to 32, in one block of 16 or two
-  const bool own_sh = x.rows > 32, p_sh = p_rows > 32;
+  // the longest walk: sink and window, each with a tile that it fills in part
+  const int64_t visible = (int64_t)x.n_init + x.n_local + x.n_new + 2 * SHARED_TILE, seen = visible < x.capacity ? visible : x.capacity;
+  const bool ragged = x.batch > 1 && seen == x.capacity;               // walks of lengths that the host does not know
+  // Rows that the workers take: up to 32, in one block of 16 or two.  With two a wave has its SIMD to itself, and where
+  // the walks are alike in length waves that share tiles are faster: 20 rows, 4 heads of 40K, 30 -> 26 us, 32 sequences
+  // with windows of 5K, 69 -> 61 (8 heads of 128K the same); 32 sequences of up to 32K, 198 -> 229.
+  const bool own_sh = x.rows > 32 || (x.rows > 16 && !prefix && !ragged), p_sh = p_rows > 32;
   // (of a prefix of more than 128 rows only a rest of less than 64 slots)
   const int64_t most = own_sh ? (p_sh ? 0 : p_rows) : p_sh || p_rows < x.rows ? x.rows : p_rows;
   x.row_blocks = most <= 16 ? 1 : 2;
@@ -139,13 +144,10 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   x.p_row_tiles = p_sh && p_rows <= 128 ? 0 : (int32_t)((p_rows + tile_rows - 1) / tile_rows);
   x.slot_rows = prefix || x.rows > tile_rows ? tile_rows : x.rows;
   x.direct = !prefix;
-  // the longest walk: sink and window, each with a tile that it fills in part
-  const int64_t visible = (int64_t)x.n_init + x.n_local + x.n_new + 2 * SHARED_TILE, seen = visible < x.capacity ? visible : x.capacity;
   x.max_tiles = (int32_t)((seen + CACHE_TILE - 1) / CACHE_TILE);
   int64_t segments = (int64_t)x.batch * x.n_kv * x.row_tiles;
   int64_t places = segments * (x.max_tiles + SEGMENT_COST);
-  if (own_sh) plan_shared(x.own_sh, (int64_t)x.batch * x.n_kv, x.rows, (seen + SHARED_TILE - 1) / SHARED_TILE, false,
-                          x.batch > 1 && seen == x.capacity);
+  if (own_sh) plan_shared(x.own_sh, (int64_t)x.batch * x.n_kv, x.rows, (seen + SHARED_TILE - 1) / SHARED_TILE, false, ragged);
   if (prefix) {
     x.pk = static_cast<const bf16_t *>(prefix->k); x.pv = static_cast<const bf16_t *>(prefix->v);
     x.p_lens = prefix->lens;

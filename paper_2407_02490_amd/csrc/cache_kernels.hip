@@ -5,7 +5,7 @@
 //
 // Every key costs 512 bytes and, with R rows per K/V head, 512 R flops: up to some hundred rows the memory bounds
 // it, so the kernels are built to keep loads in flight.
-// Up to 32 rows (cache_attn_kernel): a wave is a worker of its own.  It takes a consecutive share of the tiles of
+// Up to 16 rows, or 32 (cache_attn_kernel): a wave is a worker of its own.  It takes a consecutive share of the tiles of
 // all sequences (cache_walk.h), fetches tile t+1 into its half of an LDS ring (global -> LDS, no registers) while it
 // computes tile t, and meets no barrier.  Rows are the columns of 16x16x32 MFMAs (S^T = K Q^T, O^T += V^T P^T): the
 // accumulator layout of S^T is the operand layout that the second product needs, so P never leaves registers.
@@ -678,7 +678,7 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
   }
 }
 
-// ---- more than 32 rows -----------------------------------------------------------------------------------
+// ---- many rows (from 17 or 33 on) -----------------------------------------------------------------------
 // Eight waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile): four take the
 // first 32 keys and four the others, 16 NB rows each, 64 or 128 rows a workgroup; at the end the two halves' sums are
 // joined in LDS.  So a SIMD has two waves, one's exponentials beside the other's products, and no operand is read from

@@ -239,7 +239,7 @@ struct CacheCall {
   int32_t rows, row_tiles;              // rows of a K/V head (group * n_new), in tiles of 16 row_blocks
   int32_t p_cap, p_row_tiles;           // capacity of the prefix (0: none), row tiles of its batch * rows rows
   int32_t row_blocks, workers, max_tiles, slot_rows;
-  SharedPart own_sh, p_sh;              // more than 32 rows: not for the workers
+  SharedPart own_sh, p_sh;              // rows that are not for the workers: own, of the prefix
   int32_t direct;                       // O of a whole segment is final (no prefix)
   float c_log2;
   // workspace

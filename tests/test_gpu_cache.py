@@ -232,6 +232,19 @@ def test_segments_that_one_workgroup_takes_whole(B, case, mode):
     check_attention(q, cache, o, n_init, n_local, before=before if mode else None)
 
 
+@pytest.mark.parametrize("case", [(1, 4, 1, 16, 3000, [2990], 0, BIG), (2, 8, 2, 10, 1400, [1400, 333], 100, 500), (3, 33, 1, 1, 700, [700, 3, 64], 0, BIG)],
+                         ids=["64", "40", "33"])
+def test_up_to_64_rows_have_p_in_two_parts(B, case):
+    """The bound of few rows, which P in one bf16 would not keep, for 33 to 64 rows too."""
+    batch, hq, hkv, T, cap, lens, n_init, n_local = case
+    cache = cache_of(B, 47, batch, hkv, cap, lens)
+    q = queries(47, batch, hq, T)
+    o = attend(B, q, cache, n_init, n_local)
+    for b, n in enumerate(lens):
+        want, _, mag, slack = R.attention(R.f64(q)[b], R.f64(cache.k)[b], R.f64(cache.v)[b], n, n_init, n_local, None, None, None)
+        R.check_o(o[b], want, mag, slack, f"sequence {b} ({n} tokens)", R.P_TWO_BF16)
+
+
 def test_output_in_place_of_many_query_rows(B):
     """o = q with 128 rows and several workgroups a row; with weights, which need q once more, it is refused."""
     cache = cache_of(B, 43, 1, 2, 9000, [8990])
