@@ -1099,25 +1099,27 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void cache_join_kernel(CacheCall x
 }
 
 // Weights of more than 16 rows, whose logits would be more bytes than the keys: they are computed anew.  A wave takes
-// 64 keys (K as A operands, in registers) and all rows, 16 at a time; per row block 16 MFMAs and 16 exponentials a
+// 16 KT keys (K as A operands, in registers) and all rows, 16 at a time; per row block 4 KT MFMAs and 4 KT exponentials a
 // lane.  The four waves of a workgroup share the rows: each brings one of four blocks into LDS, as operands, while
 // the four before are used.  (Every wave with loads of its own: 256 rows, 4 heads of 40K tokens, 35 us, half of it
 // for the loads.)
-constexpr int COLUMN_KEYS = 256;                                // per workgroup
+// KT = 2 where that gives 512 workgroups, two per CU, 1 otherwise, when the time is a wave's latency: the call with 256 rows,
+// 4 heads of 40K, 74 and 82 us (KT = 4: 76), the kernel with 464 rows, 8 heads of 511 tokens, 17 and 16 (28).
+template <int KT>
 __global__ __launch_bounds__(256, 3) void cache_column_kernel(CacheCall x) {
   __shared__ bf16x8 rows_q[2][4][4][64];                        // [buffer][row block][k step][lane]
   __shared__ float rows_m[2][64];
   const int kvh = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
-  const int n = lane & 15, g = lane >> 4, kb = blockIdx.x * COLUMN_KEYS + wave * 64;
+  const int n = lane & 15, g = lane >> 4, kb = blockIdx.x * (64 * KT) + wave * (16 * KT);
   const int len = uni(min(max(x.lens[b], 0), x.capacity)), i0 = len - x.n_new;
-  if ((int)blockIdx.x * COLUMN_KEYS >= len) return;
+  if ((int)blockIdx.x * (64 * KT) >= len) return;
   const int64_t head = (int64_t)b * x.n_kv + kvh;
   // every row sees every key / no row sees a key
-  const bool whole = kb + 63 <= i0 && (kb + 63 < x.n_init || len - 1 - kb < x.n_local);
-  const bool hidden = kb >= len || (kb >= x.n_init && i0 - (kb + 63) >= x.n_local);
-  bf16x8 k[4][4];                                               // [16 keys][k step]
+  const bool whole = kb + 16 * KT - 1 <= i0 && (kb + 16 * KT - 1 < x.n_init || len - 1 - kb < x.n_local);
+  const bool hidden = kb >= len || (kb >= x.n_init && i0 - (kb + 16 * KT - 1) >= x.n_local);
+  bf16x8 k[KT][4];                                               // [16 keys][k step]
 #pragma unroll
-  for (int kt = 0; kt < 4; ++kt) {
+  for (int kt = 0; kt < KT; ++kt) {
     const bf16_t *row = x.k + b * x.k_sb + kvh * x.k_sh + (int64_t)min(kb + 16 * kt + n, len - 1) * x.k_st + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) k[kt][ks] = *reinterpret_cast<const bf16x8 *>(row + 32 * ks);
@@ -1138,9 +1140,9 @@ __global__ __launch_bounds__(256, 3) void cache_column_kernel(CacheCall x) {
     for (int ks = 0; ks < 4; ++ks) rows_q[buf][wave][ks][lane] = q[ks];
     if (g == 0) rows_m[buf][16 * wave + n] = m;
   };
-  float sum[16];
+  float sum[4 * KT];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+  for (int i = 0; i < 4 * KT; ++i) sum[i] = 0.f;
   load(0);
   store(0);
   __syncthreads();
@@ -1149,24 +1151,24 @@ __global__ __launch_bounds__(256, 3) void cache_column_kernel(CacheCall x) {
     if (more) load(r0 + 64);
     for (int blk = 0; blk < 4 && r0 + 16 * blk < x.rows && !hidden; ++blk) {
       const float ref = rows_m[buf][16 * blk + n];
-      f32x4 s[4];
+      f32x4 s[KT];
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
         const bf16x8 qf = rows_q[buf][blk][ks][lane];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
+        for (int kt = 0; kt < KT; ++kt) {
           const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
           s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][ks], qf, ks == 0 ? zero : s[kt], 0, 0, 0);
         }
       }
       if (whole) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum[i] += fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -ref));
+        for (int i = 0; i < 4 * KT; ++i) sum[i] += fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -ref));
         continue;
       }
       const int t = min(r0 + 16 * blk + n, x.rows - 1) / x.group;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 4 * KT; ++i) {
         const bool sees = cache_visible(kb + 16 * (i >> 2) + 4 * g + (i & 3), i0 + t, x.n_init, x.n_local);
         const float p = fast_exp2(fmaf(s[i >> 2][i & 3], x.c_log2, -ref));
         sum[i] += sees ? p : 0.f;
@@ -1176,13 +1178,13 @@ __global__ __launch_bounds__(256, 3) void cache_column_kernel(CacheCall x) {
     __syncthreads();
   }
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
+  for (int i = 0; i < 4 * KT; ++i)
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) sum[i] += __shfl_xor(sum[i], d);
   if (n != 0) return;
   float *to = x.weight + b * x.w_sb + kvh * x.w_sh;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 4 * KT; ++i) {
     const int key = kb + 16 * (i >> 2) + 4 * g + (i & 3);
     if (key < len) to[key] = x.add_weights ? to[key] + sum[i] : sum[i];
   }
@@ -1594,7 +1596,9 @@ hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {
     else four ? join(cache_join_kernel<4, false>) : join(cache_join_kernel<1, false>);
   }
   if ((e = hipGetLastError()) != hipSuccess || !x.weight || x.logits) return e;
-  hipLaunchKernelGGL(cache_column_kernel, dim3((x.capacity + COLUMN_KEYS - 1) / COLUMN_KEYS, x.n_kv, x.batch), dim3(256), 0, st, x);
+  const int wide = (x.capacity + 127) / 128;
+  if (wide * x.n_kv * x.batch >= 512) hipLaunchKernelGGL(cache_column_kernel<2>, dim3(wide, x.n_kv, x.batch), dim3(256), 0, st, x);
+  else hipLaunchKernelGGL(cache_column_kernel<1>, dim3((x.capacity + 63) / 64, x.n_kv, x.batch), dim3(256), 0, st, x);
   return hipGetLastError();
 }
 
