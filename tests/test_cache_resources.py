@@ -1,5 +1,5 @@
 """What the compiler reports of the cache kernels in libminf.so."""
-from test_kernel_resources import kernels  # noqa: F401  (a fixture)
+from tests.test_kernel_resources import kernels  # noqa: F401  (a fixture)
 
 
 def test_cache_kernels_use_no_scratch_memory(kernels):  # noqa: F811
