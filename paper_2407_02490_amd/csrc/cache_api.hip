@@ -81,6 +81,11 @@ struct Plan {
   size_t need, at_ml, at_shared[2], at_shared_ml[2], at_stat, at_logits;     // [0] own, [1] prefix
 };
 
+// Segments of so few tiles that one workgroup each, all at a time, ends sooner than parts and their join.  (32 heads of
+// 128, 256 and 512 keys, 24 rows: 14.2, 14.5, 15.1 us in parts, 8.4, 10.1, 13.4 whole; 80 rows: 16.6, 17.8, 18.8 and 11.2,
+// 13.0, 17.9; 240 rows of 256 and 512 keys: 26.7, 29.1 and 14.8, 19.6.)
+bool brief(int64_t segments, int64_t tiles) { return segments <= CUS && tiles <= 8; }
+
 // How the rows of `heads` K/V heads (of a sequence) are taken, whole: 256 at a time: row tiles, and parts such that the
 // workgroups, one per CU, come in rounds of least time.  A workgroup's start and end cost as much as six tiles.
 // ragged: the tiles are those of a full cache, of several sequences whose lengths the host does not know.  Then the time
@@ -135,7 +140,13 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   // Rows that the workers take: up to 32, in one block of 16 or two.  With two a wave has its SIMD to itself, and where
   // the walks are alike in length waves that share tiles are faster: 20 rows, 4 heads of 40K, 30 -> 26 us, 32 sequences
   // with windows of 5K, 69 -> 61 (8 heads of 128K the same); 32 sequences of up to 32K, 198 -> 229.
-  const bool own_sh = x.rows > 32 || (x.rows > 16 && !prefix && !ragged), p_sh = p_rows > 32;
+  // So they are, of up to 64 rows, where a workgroup per K/V head and sequence takes it whole in no more time than the
+  // launch of the join does (brief(); with weights that launch gives them as well): 8 heads of 64, 256 and 512 keys,
+  // 4 rows each, 12.0, 12.4, 12.3 us by workers, 7.0, 8.9, 12.4 by one workgroup; 256 heads 13.7, 18.4, 24.1 and 7.6, 12.4, 16.9.
+  const int64_t own_tiles = (seen + SHARED_TILE - 1) / SHARED_TILE, own_heads = (int64_t)x.batch * x.n_kv;
+  const bool own_sh = x.rows > 32 || (x.rows > 16 && !prefix && !ragged) ||
+                      (x.rows <= 64 && !prefix && weights == MINF_WEIGHTS_NONE && brief(own_heads, own_tiles));
+  const bool p_sh = p_rows > 32;
   // (of a prefix of more than 128 rows only a rest of less than 64 slots)
   const int64_t most = own_sh ? (p_sh ? 0 : p_rows) : p_sh || p_rows < x.rows ? x.rows : p_rows;
   x.row_blocks = most <= 16 ? 1 : 2;
@@ -147,7 +158,8 @@ minf_status make_plan(const minf_queries *q, const minf_kv_cache *c, const minf_
   x.max_tiles = (int32_t)((seen + CACHE_TILE - 1) / CACHE_TILE);
   int64_t segments = (int64_t)x.batch * x.n_kv * x.row_tiles;
   int64_t places = segments * (x.max_tiles + SEGMENT_COST);
-  if (own_sh) plan_shared(x.own_sh, (int64_t)x.batch * x.n_kv, x.rows, (seen + SHARED_TILE - 1) / SHARED_TILE, false, ragged);
+  if (own_sh) plan_shared(x.own_sh, own_heads, x.rows, own_tiles, false, ragged);
+  if (own_sh && !prefix && brief(own_heads * x.own_sh.row_tiles, own_tiles)) x.own_sh.splits = 1;
   if (prefix) {
     x.pk = static_cast<const bf16_t *>(prefix->k); x.pv = static_cast<const bf16_t *>(prefix->v);
     x.p_lens = prefix->lens;
