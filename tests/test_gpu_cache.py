@@ -592,3 +592,35 @@ def test_on_another_stream(B):
     B.minf_cache_attn(q, o, cache, ws, weights="set", stream=s)
     s.synchronize()
     assert torch.equal(o, want) and torch.equal(w, cache.weight)
+
+
+@pytest.mark.parametrize("T", [1, 16], ids=["8-rows", "128-rows"])
+def test_two_graphs_at_once(B, T):
+    """Two captured calls on the same K and V, each with weights and a workspace of its own, replayed side by side on two
+    streams, then the other way round, with eager calls in between."""
+    shared = cache_of(B, 48, 2, 2, 3000, [2900, 1700])
+    caches = [B.KVCache(shared.k, shared.v, shared.lens, torch.zeros(2, 2, 3000, device="cuda")) for _ in range(2)]
+    qs = [queries(48 + i, 2, 16, T) for i in range(2)]
+    want = [(attend(B, qs[i], caches[i], weights="set"), caches[i].weight.clone()) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty_like(q) for q in qs]
+    ws = [workspace(B.minf_cache_attn_workspace_bytes(qs[i], caches[i], weights="set")) for i in range(2)]
+    graphs = []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        streams[i].wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graphs[i], stream=streams[i]):
+            B.minf_cache_attn(qs[i], outs[i], caches[i], ws[i], weights="set")
+    for turn in range(4):
+        for o, c in zip(outs, caches):
+            o.zero_()
+            c.weight.zero_()
+        torch.cuda.synchronize()
+        for i in (0, 1) if turn % 2 == 0 else (1, 0):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(outs[i].view(torch.int16), want[i][0].view(torch.int16)), f"turn {turn} graph {i}"
+            assert torch.equal(caches[i].weight, want[i][1]), f"turn {turn} graph {i}"
+        attend(B, qs[turn % 2], shared)
