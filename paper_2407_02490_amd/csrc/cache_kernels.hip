@@ -682,14 +682,17 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
 // Eight waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile): four take the
 // first 32 keys and four the others, 16 NB rows each, 64 or 128 rows a workgroup; at the end the two halves' sums are
 // joined in LDS.  So a SIMD has two waves, one's exponentials beside the other's products, and no operand is read from
-// LDS more often than with four.  Memory bounds 128 rows (32 KiB a tile take a CU 1.4 us), the arithmetic more of them.
+// LDS more often than with four.  The barrier of every tile would keep both in the same phase; priority pulls them apart:
+// of a prefix the first half's waves have it, else the wave in its exponentials (the calls of the two sizes below,
+// neither 137 and 74.3 us, the first half 130 and 73.9, the exponentials 133 and 73.5).
+// Memory bounds 128 rows (32 KiB a tile take a CU 1.4 us), the arithmetic more of them.
 // (128 rows, 8 heads of 128K tokens, and 256 rows, 4 heads of 40K: 110 and 39 us; four waves with all 64 keys 120 and
 // 44; two workgroups of four waves and 32-key tiles a CU 109 and 39, but twice the pieces to join, 3 us more; eight
 // waves of 16 rows, which read every operand twice as often, 132 us for the 128 rows; the 256-row loop of
 // cache_prefix_kernel 142.)
 // P in two bf16 up to 64 rows.  Beyond in one, as in the prefill kernels: off by 2^-8 of a probability at most, which is
-// what O itself is rounded by, and the errors of many keys cancel in part; its rest would take the matrix cores as long
-// again as the product with V.
+// what O itself is rounded by, and the errors of many keys cancel in part; the product of its rest would cost the same two
+// calls 27 and 8 us.
 // A workgroup takes one part (of x.*_sh.splits) of the tiles that its rows see; a segment in one part is final, of
 // others reference, sum and unnormalised O go to the workspace for cache_join_kernel.
 // Launch order: the row tiles that read the same slots run on one XCD, one after the other.
@@ -771,6 +774,7 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
   CacheLane lo;
   lo.init(lane);
   const float c_log2 = x.c_log2;
+  if (PREFIX && half == 0) __builtin_amdgcn_s_setprio(1);
   for (int i = 0; i < n; ++i) {
     MINF_WAIT_VMCNT(8);                        // this wave's part of tile i; those of i + 1 and i + 2 may run
     __syncthreads();                           // all of tile i is there; all waves are done with tile i - 1
@@ -789,6 +793,7 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
           s[kt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, st.q.q[nb][ks], ks == 0 ? zero : s[kt][nb], 0, 0, 0);
         }
       }
+    if (!PREFIX) __builtin_amdgcn_s_setprio(1);
     const bool edge = !mask.whole<CACHE_TILE>(kb);
     if (edge) {
 #pragma unroll
@@ -840,6 +845,7 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
       }
       st.l[nb] += sum;
     }
+    if (!PREFIX) __builtin_amdgcn_s_setprio(0);
     if (!PREFIX && edge && mask.n_tok > 1 && tile_not_finite<HALF_BYTES>(tV, lane)) {
       update_by_token<NB, PARTS>(st, p, tV, lds + SHARED_RING + wave * SHARED_ROOM, kb, mask, lane);
     } else {
