@@ -679,27 +679,32 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
 }
 
 // ---- many rows (from 17 or 33 on) -----------------------------------------------------------------------
-// Eight waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile): four take the
-// first 32 keys and four the others, 16 NB rows each, 64 or 128 rows a workgroup; at the end the two halves' sums are
-// joined in LDS.  So a SIMD has two waves, one's exponentials beside the other's products, and no operand is read from
+// HALVES = 2: eight waves share 64-key tiles (a ring of four: loads go out three tiles ahead, one barrier a tile); four
+// take the first 32 keys and four the others, 16 NB rows each, 64 or 128 rows a workgroup; at the end the two halves' sums
+// are joined in LDS.  So a SIMD has two waves, one's exponentials beside the other's products, and no operand is read from
 // LDS more often than with four.  The barrier of every tile would keep both in the same phase; priority pulls them apart:
 // of a prefix the first half's waves have it, else the wave in its exponentials (the calls of the two sizes below,
 // neither 137 and 74.3 us, the first half 130 and 73.9, the exponentials 133 and 73.5).
+// HALVES = 1: four waves, 32-key tiles, two workgroups a CU, which overlap each other's starts and ends.  Taken of 128 rows
+// a workgroup where there are more workgroups than CUs (4 heads of 32 sequences of 32K, 128 and 256 rows: 479 and 842 us with
+// two halves, 438 and 784 with one; of up to 32K 282 and 492, 288 and 457; 64 rows 409 and 391, 126 short sequences 98 and 100).
 // Memory bounds 128 rows (32 KiB a tile take a CU 1.4 us), the arithmetic more of them.
-// (128 rows, 8 heads of 128K tokens, and 256 rows, 4 heads of 40K: 110 and 39 us; four waves with all 64 keys 120 and
-// 44; two workgroups of four waves and 32-key tiles a CU 109 and 39, but twice the pieces to join, 3 us more; eight
-// waves of 16 rows, which read every operand twice as often, 132 us for the 128 rows; the 256-row loop of
-// cache_prefix_kernel 142.)
+// (128 rows, 8 heads of 128K tokens, and 256 rows, 4 heads of 40K: 107 and 37 us; four waves with all 64 keys 120 and
+// 44; HALVES = 1 109 and 39, and twice the pieces to join, 3 us more; eight waves of 16 rows, which read every operand
+// twice as often, 132 us for the 128 rows; the 256-row loop of cache_prefix_kernel 142.)
 // P in two bf16 up to 64 rows.  Beyond in one, as in the prefill kernels: off by 2^-8 of a probability at most, which is
 // what O itself is rounded by, and the errors of many keys cancel in part; the product of its rest would cost the same two
 // calls 27 and 8 us.
 // A workgroup takes one part (of x.*_sh.splits) of the tiles that its rows see; a segment in one part is final, of
 // others reference, sum and unnormalised O go to the workspace for cache_join_kernel.
 // Launch order: the row tiles that read the same slots run on one XCD, one after the other.
-constexpr int SHARED_WAVES = 8, SHARED_RING = 4 * 2 * TILE_BYTES, SHARED_ROOM = 4096;    // ROOM (per wave): update_by_token
-template <int NB, bool PREFIX>
-__global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(CacheCall x) {
-  constexpr int W = SHARED_WAVES / 2, PARTS = NB == 1 ? 2 : 1, prefix = PREFIX;
+constexpr int SHARED_ROOM = 4096;                                            // per wave: update_by_token
+constexpr int shared_waves(int halves) { return 4 * halves; }
+constexpr int shared_ring(int halves) { return 4 * 2 * HALF_BYTES * halves; }
+template <int NB, bool PREFIX, int HALVES>
+__global__ __launch_bounds__(64 * shared_waves(HALVES), 2) void cache_shared_kernel(CacheCall x) {
+  constexpr int KEYS = CACHE_TILE * HALVES, BYTES = HALF_BYTES * HALVES;     // of a tile
+  constexpr int W = 4, PARTS = NB == 1 ? 2 : 1, prefix = PREFIX;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = to_sgpr(threadIdx.x >> 6);
   const int half = to_sgpr(wave / W), row_wave = wave - half * W;            // of a tile's keys; of the rows
@@ -733,20 +738,21 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
   src.strides(x, prefix, lane);
   src.heads(x, c);
   const unsigned ring = uni(lds_addr_of(lds));
-  const int upper = wave & 1;
+  const int upper = wave & 1, tiles = n * (SHARED_TILE / KEYS);
+  auto base = [&](int i) { return HALVES == 2 ? w.base(t0 + i) : w.base(t0 + (i >> 1)) + CACHE_TILE * (i & 1); };
   const unsigned k0 = upper ? src.kofs[2] : src.kofs[0], k1 = upper ? src.kofs[3] : src.kofs[1];
   const unsigned v0 = upper ? src.vofs[2] : src.vofs[0], v1 = upper ? src.vofs[3] : src.vofs[1];
   auto fetch = [&](int i) {                                                  // a wave: 8 rows of K and of V
-    const unsigned to = ring + (i & 3) * (2 * TILE_BYTES);
-    const int kb = w.base(t0 + min(i, n - 1)), end = kb + SHARED_TILE;
+    const unsigned to = ring + (i & 3) * (2 * BYTES);
+    const int kb = base(min(i, tiles - 1)), end = kb + KEYS;
     if (end <= w.len && (kb >= w.lo || end <= w.e1)) {
       const int row = kb + 16 * (wave >> 1);
       const unsigned at = to_sgpr(to + 2048 * wave);
       src.rows8(src.kh + (uint64_t)(unsigned)row * src.k_rb + 2048 * upper, k0, k1, at);
-      src.rows8(src.vh + (uint64_t)(unsigned)row * src.v_rb + 2048 * upper, v0, v1, at + TILE_BYTES);
+      src.rows8(src.vh + (uint64_t)(unsigned)row * src.v_rb + 2048 * upper, v0, v1, at + BYTES);
     } else {
       src.template rows_in_part<2>(src.kh, src.k_rb, kb, 8 * wave, w, to, lane);
-      src.template rows_in_part<2>(src.vh, src.v_rb, kb, 8 * wave, w, to + TILE_BYTES, lane);
+      src.template rows_in_part<2>(src.vh, src.v_rb, kb, 8 * wave, w, to + BYTES, lane);
     }
   };
   CacheRows<NB> st;
@@ -775,12 +781,12 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
   lo.init(lane);
   const float c_log2 = x.c_log2;
   if (PREFIX && half == 0) __builtin_amdgcn_s_setprio(1);
-  for (int i = 0; i < n; ++i) {
+  for (int i = 0; i < tiles; ++i) {
     MINF_WAIT_VMCNT(8);                        // this wave's part of tile i; those of i + 1 and i + 2 may run
     __syncthreads();                           // all of tile i is there; all waves are done with tile i - 1
     fetch(i + 3);                              // behind the last tile it is repeated: every tile issues as many loads
-    const char *tK = lds + (i & 3) * (2 * TILE_BYTES) + half * HALF_BYTES, *tV = tK + TILE_BYTES;
-    const int kb = w.base(t0 + i) + CACHE_TILE * half;
+    const char *tK = lds + (i & 3) * (2 * BYTES) + half * HALF_BYTES, *tV = tK + BYTES;
+    const int kb = base(i) + CACHE_TILE * half;
     f32x4 s[2][NB];                            // [16 keys][row block]
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
@@ -847,7 +853,7 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
     }
     if (!PREFIX) __builtin_amdgcn_s_setprio(0);
     if (!PREFIX && edge && mask.n_tok > 1 && tile_not_finite<HALF_BYTES>(tV, lane)) {
-      update_by_token<NB, PARTS>(st, p, tV, lds + SHARED_RING + wave * SHARED_ROOM, kb, mask, lane);
+      update_by_token<NB, PARTS>(st, p, tV, lds + shared_ring(HALVES) + wave * SHARED_ROOM, kb, mask, lane);
     } else {
 #pragma unroll
       for (int db = 0; db < 8; ++db) {
@@ -862,30 +868,32 @@ __global__ __launch_bounds__(64 * SHARED_WAVES, 2) void cache_shared_kernel(Cach
     __builtin_amdgcn_s_waitcnt(0xC07F);        // LDS reads done
   }
   MINF_WAIT_VMCNT(0);                          // the repeated loads
-  // The two halves' sums, in the place of the ring: the same lane has the same row and the same d of both.
-  __syncthreads();
-  f32x4 *other_o = reinterpret_cast<f32x4 *>(lds) + row_wave * (NB * 8 * 64) + lane;
-  float2 *other_ml = reinterpret_cast<float2 *>(lds + W * NB * 8 * 64 * 16) + row_wave * (NB * 64) + lane;
-  if (half == 1) {
+  if (HALVES == 2) {
+    // The two halves' sums, in the place of the ring: the same lane has the same row and the same d of both.
+    __syncthreads();
+    f32x4 *other_o = reinterpret_cast<f32x4 *>(lds) + row_wave * (NB * 8 * 64) + lane;
+    float2 *other_ml = reinterpret_cast<float2 *>(lds + W * NB * 8 * 64 * 16) + row_wave * (NB * 64) + lane;
+    if (half == 1) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        other_ml[64 * nb] = float2{st.m[nb], st.l[nb]};
+#pragma unroll
+        for (int db = 0; db < 8; ++db) other_o[64 * (8 * nb + db)] = st.o[nb][db];
+      }
+    }
+    __syncthreads();
+    if (half == 1) return;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      other_ml[64 * nb] = float2{st.m[nb], st.l[nb]};
+      const float2 ml = other_ml[64 * nb];
+      const float m = fmaxf(st.m[nb], ml.x);
+      // (-inf: no key was seen, the sums are 0)
+      const float f0 = st.m[nb] == -INFINITY ? 1.f : fast_exp2(st.m[nb] - m), f1 = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - m);
+      st.m[nb] = m;
+      st.l[nb] = st.l[nb] * f0 + ml.y * f1;
 #pragma unroll
-      for (int db = 0; db < 8; ++db) other_o[64 * (8 * nb + db)] = st.o[nb][db];
+      for (int db = 0; db < 8; ++db) st.o[nb][db] = st.o[nb][db] * f0 + other_o[64 * (8 * nb + db)] * f1;
     }
-  }
-  __syncthreads();
-  if (half == 1) return;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const float2 ml = other_ml[64 * nb];
-    const float m = fmaxf(st.m[nb], ml.x);
-    // (-inf: no key was seen, the sums are 0)
-    const float f0 = st.m[nb] == -INFINITY ? 1.f : fast_exp2(st.m[nb] - m), f1 = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - m);
-    st.m[nb] = m;
-    st.l[nb] = st.l[nb] * f0 + ml.y * f1;
-#pragma unroll
-    for (int db = 0; db < 8; ++db) st.o[nb][db] = st.o[nb][db] * f0 + other_o[64 * (8 * nb + db)] * f1;
   }
   const int64_t item = ((int64_t)head * sh.row_tiles + rt) * splits + part;
 #pragma unroll
@@ -1567,21 +1575,25 @@ static hipError_t launch_workers(const CacheCall &x, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int NB, bool PREFIX>
+constexpr int SHARED_ROUND = 256;                               // workgroups that fill a CU each
+template <int NB, bool PREFIX, int HALVES>
 static hipError_t launch_shared_as(const CacheCall &x, const SharedPart &sh, hipStream_t st) {
-  const size_t lds = SHARED_RING + SHARED_WAVES * SHARED_ROOM;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_shared_kernel<NB, PREFIX>),
+  const size_t lds = shared_ring(HALVES) + shared_waves(HALVES) * SHARED_ROOM;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_shared_kernel<NB, PREFIX, HALVES>),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
   const int groups = (PREFIX ? 1 : x.batch) * x.n_kv * sh.splits;
-  hipLaunchKernelGGL((cache_shared_kernel<NB, PREFIX>), dim3((groups + 7) / 8 * 8 * sh.row_tiles), dim3(64 * SHARED_WAVES), lds, st, x);
+  hipLaunchKernelGGL((cache_shared_kernel<NB, PREFIX, HALVES>), dim3((groups + 7) / 8 * 8 * sh.row_tiles),
+                     dim3(64 * shared_waves(HALVES)), lds, st, x);
   return hipGetLastError();
 }
 template <bool PREFIX>
 static hipError_t launch_shared(const CacheCall &x, const SharedPart &sh, hipStream_t st) {
   if (!sh.on) return hipSuccess;
   if (sh.tile_rows == 256) return launch_cache_prefix(x, st);
-  return sh.tile_rows == 64 ? launch_shared_as<1, PREFIX>(x, sh, st) : launch_shared_as<2, PREFIX>(x, sh, st);
+  if (sh.tile_rows == 64) return launch_shared_as<1, PREFIX, 2>(x, sh, st);
+  if (!PREFIX && (int64_t)x.batch * x.n_kv * sh.splits * sh.row_tiles > SHARED_ROUND) return launch_shared_as<2, false, 1>(x, sh, st);
+  return launch_shared_as<2, PREFIX, 2>(x, sh, st);
 }
 
 hipError_t launch_cache_attn(const CacheCall &x, hipStream_t st) {

@@ -184,6 +184,31 @@ def test_hidden_slots_do_not_matter_to_many_rows(B, bad, T):
     assert (cache.weight[0, :, n_init:n - T - n_local + 1] == 0).all()
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("-inf")])
+def test_hidden_slots_do_not_matter_to_many_rows_of_many_heads(B, bad):
+    """The same of 80 rows and more heads than CUs."""
+    batch, T, cap, n_init, n_local = 75, 20, 200, 11, 40
+    lens = [199 - b % 7 for b in range(batch)]
+    cache, clean = (cache_of(B, 49, batch, 4, cap, lens) for _ in range(2))
+    for t in (cache.k, cache.v):
+        for b, n in enumerate(lens):
+            t[b, :, n_init:n - T - n_local + 1] = bad
+            t[b, :, n - 1] = bad
+    q = queries(49, batch, 16, T)
+    o = attend(B, q, cache, n_init, n_local)
+    clean.lens -= 1
+    check_attention(q[:, :, :T - 1], clean, o[:, :, :T - 1], n_init, n_local)
+
+
+def test_many_rows_of_many_parts(B):
+    """160 rows per K/V head, sequences of unequal lengths in several parts, more workgroups than CUs."""
+    lens = [2000, 1, 777, 1999, 64, 0, 1500, 320]
+    cache = cache_of(B, 50, 8, 4, 2000, lens, "token")
+    q = queries(50, 8, 20, 32)
+    check_attention(q, cache, attend(B, q, cache))
+    check_attention(q, cache, attend(B, q, cache, 70, 1100), 70, 1100)
+
+
 @pytest.mark.parametrize("T", [5, 12, 33])
 def test_a_hidden_value_between_the_windows_of_many_rows(B, T):
     """A slot that the first token still sees and the later ones do not (20, 48 and 132 rows)."""
