@@ -286,7 +286,7 @@ struct CacheMask {
 
 // O^T += V^T P^T for the tokens one by one, with the V rows that a token does not see as zeros: 0 * inf and
 // 0 * NaN of a slot that a row's mask excludes would otherwise reach the row.  Only tiles with a mask and
-// with such values take it, and only where there are several tokens: slots that no row sees are not loaded.  O goes
+// with such values take it, and only where there are several tokens: slots that no row sees are zeros.  O goes
 // through 4 KiB of LDS (`room`), half of its d at a time, so that this rare path costs the others no registers.
 // tV: 32 keys from kb on; P in PARTS parts.
 template <int NB, int PARTS>
@@ -316,6 +316,25 @@ __device__ inline void update_by_token(CacheRows<NB> &st, const bf16x8 (&p)[NB][
 #pragma unroll
       for (int db = 0; db < 4; ++db) st.o[nb][4 * half + db] = mine[64 * db];
     }
+}
+
+// P of two logits as PARTS bf16.  One: rounded, off by half a step, 2^-8 of P.  Two: the high part is the largest bf16
+// below P, what is left of it, at most a step (2^-7 of P's power of two), is the low part, rounded: off by 2^-16 of P.
+// Both parts of P > 0 are greater than 0, so an infinity of V stays one: with a rounded high part the rest would be 0 or
+// negative about every second time, and inf + 0 * inf or inf - inf is NaN.  (Down to P of 2^-102: a rest below 2^-126 is none.)
+// P = 0 gives two zeros.
+template <int PARTS>
+__device__ inline void split_p(f32x2 v, bf16x2 (&part)[PARTS]) {
+  if (PARTS == 1) {
+    part[0] = __builtin_convertvector(v, bf16x2);
+    return;
+  }
+  const float x = v[0], y = v[1];                              // (a bit cast of a vector's element takes the first one)
+  const unsigned a = __builtin_elementwise_sub_sat(__builtin_bit_cast(unsigned, x), 1u);
+  const unsigned b = __builtin_elementwise_sub_sat(__builtin_bit_cast(unsigned, y), 1u);
+  part[0] = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(b, a, 0x07060302u));
+  const f32x2 rest = {x - __builtin_bit_cast(float, a & 0xffff0000u), y - __builtin_bit_cast(float, b & 0xffff0000u)};
+  part[PARTS - 1] = __builtin_convertvector(rest, bf16x2);
 }
 
 // A row's exponent reference is its maximum when it was last taken; logits may outgrow it by REF_ROOM (2^16 in
@@ -382,11 +401,13 @@ __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, cons
     for (int e = 0; e < 8; e += 2) {
       const f32x2 v = {fast_exp2(fmaf(s[nb][e >> 2][e & 3], c_log2, -m)), fast_exp2(fmaf(s[nb][e >> 2][(e & 3) + 1], c_log2, -m))};
       sum += v[0] + v[1];
-      const bf16x2 hi = __builtin_convertvector(v, bf16x2);
-      const f32x2 rest = {v[0] - (float)hi[0], v[1] - (float)hi[1]};
-      const bf16x2 lw = __builtin_convertvector(rest, bf16x2);
-      p[nb][0][e] = hi[0]; p[nb][0][e + 1] = hi[1];
-      p[nb][1][e] = lw[0]; p[nb][1][e + 1] = lw[1];
+      bf16x2 two[2];
+      split_p<2>(v, two);
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        p[nb][part][e] = two[part][0];
+        p[nb][part][e + 1] = two[part][1];
+      }
     }
     st.l[nb] += sum;
   }
@@ -542,6 +563,9 @@ struct CacheSource {
 #pragma unroll
     for (int half = 0; half < 2; ++half) rows16(h + (uint64_t)(unsigned)(kb + 16 * half) * rb, ofs, lds + 4096 * half);
   }
+  // some row sees every slot kb .. end - 1
+  template <class Walk>
+  __device__ static inline bool all_seen(int kb, int end, const Walk &w) { return end <= w.len && (kb >= w.lo || end <= w.e1); }
   // BLOCKS times four rows of the tile at kb, from row `first` on, one by one: slots that no row of the call sees are
   // replaced by one that some row does
   template <int BLOCKS, class Walk>
@@ -556,9 +580,18 @@ struct CacheSource {
       dma16(h + (uint64_t)(unsigned)key * rb + ((cpos ^ swz_f(r)) << 4), lds + (first + 4 * blk) * ROW_BYTES);
     }
   }
+  // ... and, where those rows of V are there, by zeros: P = 0 times an infinity of the one that took their place is NaN
+  template <int BLOCKS, class Walk>
+  __device__ static inline void zero_unseen(char *tV, int kb, int first, const Walk &w, int lane) {
+#pragma unroll
+    for (int blk = 0; blk < BLOCKS; ++blk) {
+      const int key = kb + first + 4 * blk + (lane >> 4);
+      if (key >= w.len || (key >= w.e1 && key < w.lo))
+        *reinterpret_cast<uint4 *>(tV + (first + 4 * blk) * ROW_BYTES + 16 * lane) = uint4{0u, 0u, 0u, 0u};
+    }
+  }
   __device__ inline void fetch(int kb, const SeqWalk &w, unsigned lds, int lane) const {
-    const int end = kb + CACHE_TILE;
-    if (end <= w.len && (kb >= w.lo || end <= w.e1)) {
+    if (all_seen(kb, kb + CACHE_TILE, w)) {
       tile(kh, k_rb, kofs, kb, lds);
       tile(vh, v_rb, vofs, kb, lds + HALF_BYTES);
     } else {
@@ -650,10 +683,11 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
         src.fetch(nxt.w.base(0), nxt.w, ring_at + (slot ^ 2 * HALF_BYTES), lane);
       }
       if (more) MINF_WAIT_VMCNT(24); else MINF_WAIT_VMCNT(8);     // K has landed
+      char *tK = ring + slot;
       auto wait_v = [&]() {
         if (more) MINF_WAIT_VMCNT(16); else MINF_WAIT_VMCNT(0);
+        if (!src.all_seen(kb, kb + CACHE_TILE, cur.w)) src.zero_unseen<8>(tK + HALF_BYTES, kb, 0, cur.w, lane);
       };
-      char *tK = ring + slot;
       if (mask.whole<CACHE_TILE>(kb)) cache_tile<NB, false>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
       else cache_tile<NB, true>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
       __builtin_amdgcn_s_waitcnt(0xC07F);    // LDS reads done: the slot may be filled again
@@ -744,8 +778,8 @@ __global__ __launch_bounds__(64 * shared_waves(HALVES), 2) void cache_shared_ker
   const unsigned v0 = upper ? src.vofs[2] : src.vofs[0], v1 = upper ? src.vofs[3] : src.vofs[1];
   auto fetch = [&](int i) {                                                  // a wave: 8 rows of K and of V
     const unsigned to = ring + (i & 3) * (2 * BYTES);
-    const int kb = base(min(i, tiles - 1)), end = kb + KEYS;
-    if (end <= w.len && (kb >= w.lo || end <= w.e1)) {
+    const int kb = base(min(i, tiles - 1));
+    if (src.all_seen(kb, kb + KEYS, w)) {
       const int row = kb + 16 * (wave >> 1);
       const unsigned at = to_sgpr(to + 2048 * wave);
       src.rows8(src.kh + (uint64_t)(unsigned)row * src.k_rb + 2048 * upper, k0, k1, at);
@@ -783,6 +817,8 @@ __global__ __launch_bounds__(64 * shared_waves(HALVES), 2) void cache_shared_ker
   if (PREFIX && half == 0) __builtin_amdgcn_s_setprio(1);
   for (int i = 0; i < tiles; ++i) {
     MINF_WAIT_VMCNT(8);                        // this wave's part of tile i; those of i + 1 and i + 2 may run
+    if (!src.all_seen(base(i), base(i) + KEYS, w))
+      src.template zero_unseen<2>(lds + (i & 3) * (2 * BYTES) + BYTES, base(i), 8 * wave, w, lane);
     __syncthreads();                           // all of tile i is there; all waves are done with tile i - 1
     fetch(i + 3);                              // behind the last tile it is repeated: every tile issues as many loads
     const char *tK = lds + (i & 3) * (2 * BYTES) + half * HALF_BYTES, *tV = tK + BYTES;
@@ -839,14 +875,14 @@ __global__ __launch_bounds__(64 * shared_waves(HALVES), 2) void cache_shared_ker
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         const f32x4 &v4 = s[e >> 2][nb];
-        f32x2 v = {fast_exp2(fmaf(v4[e & 3], c_log2, -m)), fast_exp2(fmaf(v4[(e & 3) + 1], c_log2, -m))};
+        const f32x2 v = {fast_exp2(fmaf(v4[e & 3], c_log2, -m)), fast_exp2(fmaf(v4[(e & 3) + 1], c_log2, -m))};
         sum += v[0] + v[1];
+        bf16x2 two[PARTS];
+        split_p<PARTS>(v, two);
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) {
-          const bf16x2 two = __builtin_convertvector(v, bf16x2);
-          p[nb][part][e] = two[0];
-          p[nb][part][e + 1] = two[1];
-          v = f32x2{v[0] - (float)two[0], v[1] - (float)two[1]};
+          p[nb][part][e] = two[part][0];
+          p[nb][part][e + 1] = two[part][1];
         }
       }
       st.l[nb] += sum;

@@ -1,0 +1,131 @@
+"""Infinities and NaN in slots of V that a row sees, of every kernel of the cache calls: what the
+definition in 64 bits gives, sum_j p_ij v_j with p_ij > 0, in the columns that hold such a value and in the others."""
+import numpy as np
+import pytest
+import torch
+
+from tests import cache_reference as R
+from tests.test_gpu_cache import B, BIG, cache_of, queries, workspace  # noqa: F401  (B: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+# batch, query heads, K/V heads, new tokens, capacity, lengths, n_init, n_local, weights, prefix length (0: none)
+CALLS = {
+    "workers-1-row": (1, 2, 2, 1, 1500, [1490], 0, BIG, None, 0),
+    "workers-window": (1, 8, 2, 1, 1700, [1601], 40, 900, None, 0),
+    "workers-weights": (2, 8, 2, 1, 500, [490, 33], 33, 100, "set", 0),
+    "workers-4-tokens": (1, 4, 1, 4, 900, [871], 0, BIG, None, 0),
+    "workers-two-blocks": (2, 8, 2, 5, 900, [900, 4], 0, BIG, None, 0),
+    "one-workgroup": (2, 8, 2, 1, 400, [390, 1], 0, BIG, None, 0),
+    "one-workgroup-window": (1, 8, 2, 2, 800, [777], 33, 150, None, 0),
+    "shared-20": (1, 20, 1, 1, 2000, [1990], 70, 1000, None, 0),
+    "shared-40": (1, 8, 1, 5, 1400, [1390], 0, BIG, "set", 0),
+    "shared-132": (1, 4, 1, 33, 1400, [1380], 50, 700, None, 0),
+    "shared-many": (75, 16, 4, 20, 200, [199 - i % 7 for i in range(75)], 11, 40, None, 0),
+    "prefix-8": (2, 8, 2, 1, 100, [90, 1], 0, BIG, None, 1013),
+    "prefix-32": (8, 8, 2, 1, 70, [70, 1, 2, 33, 32, 31, 9, 64], 0, BIG, None, 700),
+    "prefix-40": (10, 8, 2, 1, 50, list(range(1, 11)), 0, BIG, None, 1013),
+    "prefix-100": (25, 8, 2, 1, 50, list(range(1, 26)), 0, BIG, None, 957),
+    "prefix-160": (40, 8, 2, 1, 50, list(range(1, 41)), 0, BIG, None, 1300),
+    "prefix-2-tokens": (3, 8, 1, 2, 600, [599, 2, 64], 0, BIG, None, 333),
+}
+
+
+def make(B, case, seed):  # noqa: F811
+    batch, hq, hkv, T, cap, lens, n_init, n_local, weights, P = case
+    cache = cache_of(B, seed, batch, hkv, cap, lens, weight=weights is not None)
+    prefix = cache_of(B, seed + 1, 1, hkv, P + 20, [P], weight=False) if P else None
+    return cache, prefix, queries(seed, batch, hq, T)
+
+
+def run(B, case, cache, prefix, q):  # noqa: F811
+    n_init, n_local, weights = case[6:9]
+    o = torch.full_like(q, float("nan"))
+    if prefix is not None:
+        B.minf_prefix_attn(q, o, prefix, cache, workspace(B.minf_prefix_attn_workspace_bytes(q, prefix, cache)))
+    else:
+        ws = workspace(B.minf_cache_attn_workspace_bytes(q, cache, n_init, n_local, weights))
+        B.minf_cache_attn(q, o, cache, ws, n_init=n_init, n_local=n_local, weights=weights)
+    torch.cuda.synchronize()
+    return o
+
+
+def wanted(case, cache, prefix, q):
+    """Per sequence: n and R.attention's results."""
+    hkv, n_init, n_local, P = case[2], case[6], case[7], case[9]
+    pk = pv = None
+    if P:
+        pk, pv = R.f64(prefix.k)[0][:, :P], R.f64(prefix.v)[0][:, :P]
+    qd, kd, vd = R.f64(q), R.f64(cache.k), R.f64(cache.v)
+    for b, n in enumerate(case[5]):
+        yield b, n, R.attention(qd[b], kd[b], vd[b], n, n_init, n_local, None, pk, pv)
+
+
+def p_step(case):
+    rows = case[1] // case[2] * case[3]
+    return R.P_BF16 if rows * (case[0] if case[9] else 1) > 64 else R.P_TWO_BF16
+
+
+def sees(case, n, t, j):
+    i = n - case[3] + t
+    return i >= 0 and j <= i and (j < case[6] or i - j < case[7])
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_visible_infinities(B, name):  # noqa: F811
+    """Column 2 x + s holds an infinity of sign s in the x-th of some slots, column 20 both signs in two slots, column 21
+    NaN in one: the rows that see the slot give it, the others and all other columns what they give without."""
+    case = CALLS[name]
+    batch, hq, hkv, T, cap, lens, n_init, n_local, weights, P = case
+    cache, prefix, q = make(B, case, 60)
+    first = lambda n: max(0, n - T - n_local + 1)            # the first slot of the first row's window
+    slots = [sorted({0, n // 3, min(first(n), n - 1), n - 1, max(n - T, 0)}) if n else [] for n in lens]
+    p_slots = sorted({0, 31, P // 2, P - 2, P - 1}) if P else []
+    clean = [wanted(case, cache, prefix, q)]
+    special = np.zeros((batch, T, 128), dtype=object)        # 0, "+", "-" or "nan" of each column of a row
+    want = list(clean[0])
+
+    def put(v, at, col, value):
+        v[..., at, col] = value
+
+    def mark(b, t, col, sign):
+        old = special[b, t, col]
+        special[b, t, col] = sign if old in (0, sign) else "nan"
+    plant = [(1, j, 5 + x) for x, j in enumerate(p_slots)] + [(0, None, x) for x in range(5)]
+    for is_prefix, j, x in plant:
+        for s, (value, sign) in enumerate(((float("inf"), "+"), (float("-inf"), "-"))):
+            col = 2 * x + s
+            if is_prefix:
+                put(prefix.v, j, col, value)
+            for b, n in enumerate(lens):
+                if not is_prefix:
+                    if x >= len(slots[b]):
+                        continue
+                    j = slots[b][x]
+                    put(cache.v[b], j, col, value)
+                for t in range(T):
+                    if (n - T + t >= 0) if is_prefix else sees(case, n, t, j):
+                        mark(b, t, col, sign)
+    for b, n in enumerate(lens):
+        if n >= 2:
+            for j, value, sign in ((n - 2, float("inf"), "+"), (0, float("-inf"), "-"))[n == 2:]:
+                put(cache.v[b], j, 20, value)
+                for t in range(T):
+                    if sees(case, n, t, j):
+                        mark(b, t, 20, sign)
+        if n:
+            put(cache.v[b], n - 1, 21, float("nan"))
+            for t in range(T):
+                if sees(case, n, t, n - 1):
+                    special[b, t, 21] = "nan"
+    o = R.f64(run(B, case, cache, prefix, q))
+    for b, n, (ref, w, mag, slack) in want:
+        for t in range(T):
+            plain = special[b, t] == 0
+            for sign, found in (("+", np.isposinf), ("-", np.isneginf), ("nan", np.isnan)):
+                cols = np.flatnonzero(special[b, t] == sign)
+                assert found(o[b, :, t][:, cols]).all(), f"{name}: sequence {b} token {t} columns {cols} ({sign}): {o[b, :, t][:, cols]}"
+            got = torch.from_numpy(o[b, :, t][:, plain])
+            R.check_o(got, ref[:, t][:, plain], mag[:, t][:, plain], slack[:, t], f"{name}: sequence {b} token {t}", p_step(case))
+        if weights:
+            R.check_w(cache.weight[b, :, :n], w, slack, f"{name}: weights of sequence {b}")
