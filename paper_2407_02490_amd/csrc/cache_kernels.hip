@@ -337,9 +337,9 @@ __device__ inline void split_p(f32x2 v, bf16x2 (&part)[PARTS]) {
   part[PARTS - 1] = __builtin_convertvector(rest, bf16x2);
 }
 
-// A row's exponent reference is its maximum when it was last taken; logits may outgrow it by REF_ROOM (2^16 in
-// the sums, far from any limit of fp32) before it is taken anew.  So nearly every tile needs no maximum
-// across lanes and no rescaling.
+// A row's exponent reference is its maximum when it was last taken, and REF_ROOM more: logits may outgrow that maximum by
+// so much before it is taken anew, and nearly every tile needs no maximum across lanes and no rescaling.  P is at
+// most 1 whenever (2^-16 for the maximum itself, which costs a sum in fp32 nothing): no product with V leaves fp32.
 constexpr float REF_ROOM = 16.f;
 
 // One tile of 32 keys from slot kb on.  EDGE: some row may not see some key.  keep: the logits are wanted (one
@@ -372,7 +372,7 @@ __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, cons
     float mx = s[nb][0][0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[nb][e >> 2][e & 3]);
-    outgrown = outgrown || mx * c_log2 > st.m[nb] + REF_ROOM;
+    outgrown = outgrown || mx * c_log2 > st.m[nb];
   }
   if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
 #pragma unroll
@@ -382,7 +382,7 @@ __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, cons
       for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[nb][e >> 2][e & 3]);
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32)) * c_log2;
-      const float m_new = fmaxf(st.m[nb], mx);
+      const float m_new = fmaxf(st.m[nb], mx + REF_ROOM);
       const float f = m_new == -INFINITY ? 1.f : fast_exp2(st.m[nb] - m_new);
       st.m[nb] = m_new;
       st.l[nb] *= f;
@@ -852,14 +852,14 @@ __global__ __launch_bounds__(64 * shared_waves(HALVES), 2) void cache_shared_ker
       mx[nb] = s[0][nb][0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) mx[nb] = fmaxf(mx[nb], s[e >> 2][nb][e & 3]);
-      outgrown = outgrown || mx[nb] * c_log2 > st.m[nb] + REF_ROOM;
+      outgrown = outgrown || mx[nb] * c_log2 > st.m[nb];
     }
     if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         float most = fmaxf(mx[nb], __shfl_xor(mx[nb], 16));
         most = fmaxf(most, __shfl_xor(most, 32)) * c_log2;
-        const float m_new = fmaxf(st.m[nb], most);
+        const float m_new = fmaxf(st.m[nb], most + REF_ROOM);
         const float f = m_new == -INFINITY ? 1.f : fast_exp2(st.m[nb] - m_new);
         st.m[nb] = m_new;
         st.l[nb] *= f;

@@ -1,4 +1,4 @@
-"""Infinities and NaN in slots of V that a row sees, of every kernel of the cache calls: what the
+"""Infinities, NaN and very large values in slots of V that a row sees, of every kernel of the cache calls: what the
 definition in 64 bits gives, sum_j p_ij v_j with p_ij > 0, in the columns that hold such a value and in the others."""
 import numpy as np
 import pytest
@@ -129,3 +129,39 @@ def test_visible_infinities(B, name):  # noqa: F811
             R.check_o(got, ref[:, t][:, plain], mag[:, t][:, plain], slack[:, t], f"{name}: sequence {b} token {t}", p_step(case))
         if weights:
             R.check_w(cache.weight[b, :, :n], w, slack, f"{name}: weights of sequence {b}")
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_visible_values_near_the_largest(B, name):  # noqa: F811
+    """V of up to 2^126 where a tile's logits lie above all earlier ones: no partial sum may leave fp32.  Per row at most
+    four such values are visible, of one sign in a column, so that sum_j p_ij |v_j| < 2^128 for any p_ij <= 1."""
+    case = CALLS[name]
+    lens, P = case[5], case[9]
+    cache, prefix, q = make(B, case, 70)
+    q[:] = q[:, :1, :1]                                      # one direction for every row of a sequence ...
+    if P:
+        q[:] = q[:1]                                         # ... and for all that share the prefix
+    scale = 1.0 / np.sqrt(128.0)
+
+    def lift(k, n, qb):
+        """Logits of 0, but in the last quarter of the slots 10 (base e), 14.4 in base 2."""
+        if n < 4:
+            return
+        d = qb[0, 0].float()
+        k[:, :n] = 0.1 * k[:, :n]
+        k[:, n - n // 4:n] = (k[:, n - n // 4:n].float() + d * (10.0 / scale / float(d @ d))).to(torch.bfloat16)
+    big = 2.0 ** 126
+    for b, n in enumerate(lens):
+        lift(cache.k[b], n, q[b])
+        if n >= 4:
+            cache.v[b, :, n - 1, 3] = big
+            cache.v[b, :, n - n // 4, 4] = -big
+            cache.v[b, :, 0, 5] = big
+    if P:
+        lift(prefix.k[0], P, q[0])
+        prefix.v[0, :, P - 1, 3] = big
+        prefix.v[0, :, P - P // 4 + 1, 4] = -big
+        prefix.v[0, :, 0, 6] = big
+    o = run(B, case, cache, prefix, q)
+    for b, n, (ref, w, mag, slack) in wanted(case, cache, prefix, q):
+        R.check_o(o[b], ref, mag, slack, f"{name}: sequence {b}", p_step(case))
