@@ -343,7 +343,7 @@ __device__ inline void split_p(f32x2 v, bf16x2 (&part)[PARTS]) {
 constexpr float REF_ROOM = 16.f;
 
 // One tile of 32 keys from slot kb on.  EDGE: some row may not see some key.  keep: the logits are wanted (one
-// block of rows).  wait_v awaits the V tile (the K tile is there).
+// block of rows).  wait_v awaits the V tile (the K tile is there); of an EDGE tile it clears the slots that no row sees.
 template <int NB, bool EDGE, class WaitV>
 __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, const CacheLane &lo, float c_log2, int kb,
                                   char *tK, const char *tV, bool keep, CacheLogits &out, int lane, WaitV wait_v) {
@@ -411,7 +411,7 @@ __device__ inline void cache_tile(const CacheMask &mask, CacheRows<NB> &st, cons
     }
     st.l[nb] += sum;
   }
-  wait_v();
+  wait_v(EDGE);
   if (EDGE && mask.n_tok > 1 && tile_not_finite<HALF_BYTES>(tV, lane)) {
     update_by_token<NB, 2>(st, p, tV, tK, kb, mask, lane);
   } else {
@@ -580,14 +580,18 @@ struct CacheSource {
       dma16(h + (uint64_t)(unsigned)key * rb + ((cpos ^ swz_f(r)) << 4), lds + (first + 4 * blk) * ROW_BYTES);
     }
   }
-  // ... and, where those rows of V are there, by zeros: P = 0 times an infinity of the one that took their place is NaN
+  // ... and, where those rows of V are there, by zeros: P = 0 times an infinity of the one that took their place is NaN.
+  // (Nothing of this may be kept in registers through a loop over tiles, which nearly never takes it: with the zeros and
+  // addresses held the tile loop of 128 rows had its operands read one by one, the prefix of 128K 101 -> 116 us.)
   template <int BLOCKS, class Walk>
   __device__ static inline void zero_unseen(char *tV, int kb, int first, const Walk &w, int lane) {
+    unsigned zero = 0;
+    asm volatile("" : "+v"(zero), "+v"(lane));
 #pragma unroll
     for (int blk = 0; blk < BLOCKS; ++blk) {
       const int key = kb + first + 4 * blk + (lane >> 4);
       if (key >= w.len || (key >= w.e1 && key < w.lo))
-        *reinterpret_cast<uint4 *>(tV + (first + 4 * blk) * ROW_BYTES + 16 * lane) = uint4{0u, 0u, 0u, 0u};
+        *reinterpret_cast<uint4 *>(tV + (first + 4 * blk) * ROW_BYTES + 16 * lane) = uint4{zero, zero, zero, zero};
     }
   }
   __device__ inline void fetch(int kb, const SeqWalk &w, unsigned lds, int lane) const {
@@ -684,9 +688,9 @@ __global__ __launch_bounds__(64 * CACHE_WAVES, NB == 1 ? 2 : 1) void cache_attn_
       }
       if (more) MINF_WAIT_VMCNT(24); else MINF_WAIT_VMCNT(8);     // K has landed
       char *tK = ring + slot;
-      auto wait_v = [&]() {
+      auto wait_v = [&](bool edge) {
         if (more) MINF_WAIT_VMCNT(16); else MINF_WAIT_VMCNT(0);
-        if (!src.all_seen(kb, kb + CACHE_TILE, cur.w)) src.zero_unseen<8>(tK + HALF_BYTES, kb, 0, cur.w, lane);
+        if (edge && !src.all_seen(kb, kb + CACHE_TILE, cur.w)) src.zero_unseen<8>(tK + HALF_BYTES, kb, 0, cur.w, lane);
       };
       if (mask.whole<CACHE_TILE>(kb)) cache_tile<NB, false>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
       else cache_tile<NB, true>(mask, st, lo, c_log2, kb, tK, tK + HALF_BYTES, keep, out, lane, wait_v);
