@@ -270,7 +270,9 @@ minf_status minf_dense_attn(const minf_qkv *x, const int32_t *heads, int32_t n_h
  * layer.  A value in a slot that the mask hides from a row (NaN and infinities
  * too) does not reach that row; an infinity of V in one that it sees makes that
  * element of O infinite (both signs, or a probability below 2^-80 of the row's
- * largest: NaN).  Logits, sums and O are fp32; the probabilities
+ * largest: NaN).  Finite values of V give a finite O where the magnitudes of a
+ * column's visible ones sum to less than 2^128 (O is divided by the sum of the
+ * exponentials at the end).  Logits, sums and O are fp32; the probabilities
  * multiply V as two bf16 (high and low part), those of more than 64 rows per K/V
  * head (for a prefix: of the batch) as one, as in the prefill.  Results are the
  * same bits from call to call; where a sequence's sums are cut depends on the

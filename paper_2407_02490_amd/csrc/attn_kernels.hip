@@ -2976,7 +2976,15 @@ __global__ __launch_bounds__(256) void cache_prefix_kernel(CacheCall x) {
   mp.q0 = 1 << 30; mp.lo = 0; mp.hi = 1 << 30; mp.n_init = 0; mp.n_local = (1 << 30) + BQ;
   bool has_ref = false;
   ashape_pass_pipelined<AllCls>(c, d, st, qa, has_ref, lo, mp, AllCls(), lane);
-  if (__syncthreads_or(needs_exact(st) ? 1 : 0)) {
+  // P may have exceeded 1 by far, and P V fp32: the exact scheme has P <= 1.  (0 * O: NaN of an infinity or NaN.)
+  float zero = 0.f;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) zero = fmaf(st.o[db][nb][r], 0.f, zero);
+  if (__syncthreads_or(needs_exact(st) || zero != 0.f ? 1 : 0)) {
     load_rows();
     reset_for_max_pass(st);
     ashape_pass<PASS_MAX>(c, st, lo, mp, wave, lane);

@@ -165,3 +165,29 @@ def test_visible_values_near_the_largest(B, name):  # noqa: F811
     o = run(B, case, cache, prefix, q)
     for b, n, (ref, w, mag, slack) in wanted(case, cache, prefix, q):
         R.check_o(o[b], ref, mag, slack, f"{name}: sequence {b}", p_step(case))
+
+
+@pytest.mark.parametrize("flip", [False, True], ids=["rising", "falling"])
+def test_large_values_behind_a_prefix_whose_logits_outgrow_their_first_tile(B, flip):  # noqa: F811
+    """160 rows: logits that rise by 60 (base 2) over the tiles that one workgroup takes, times V of 2^100."""
+    P, batch = 20480, 20
+    cache = cache_of(B, 80, batch, 8, 32, [1 + i for i in range(batch)], weight=False)
+    q = queries(80, batch, 64, 1)
+    q[:] = q[:1, :1]
+    d = q[0, 0, 0].float()
+    ramp = torch.arange(P, device="cuda") % 640 / 640.0 * 60.0 * float(np.log(2.0)) * float(np.sqrt(128.0)) / float(d @ d)
+    if flip:
+        ramp = ramp.flip(0)
+    k = (ramp[:, None] * d[None]).to(torch.bfloat16).expand(1, 8, P, 128)
+    g = torch.Generator("cuda").manual_seed(80)
+    v = (torch.randn(1, 8, P, 128, generator=g, device="cuda") * 2.0 ** 100).to(torch.bfloat16)
+    prefix = B.KVCache(k, v, torch.tensor([P], dtype=torch.int32, device="cuda"))
+    o = torch.full_like(q, float("nan"))
+    B.minf_prefix_attn(q, o, prefix, cache, workspace(B.minf_prefix_attn_workspace_bytes(q, prefix, cache)))
+    torch.cuda.synchronize()
+    pk, pv = R.f64(k)[0], R.f64(v)[0]
+    qd, kd, vd = R.f64(q), R.f64(cache.k), R.f64(cache.v)
+    for b in (0, 7, 19):
+        heads = slice(0, 64, 8)                              # one query head of each group: all rows are alike
+        ref, _, mag, slack = R.attention(qd[b][heads], kd[b], vd[b], 1 + b, 0, BIG, None, pk, pv)
+        R.check_o(o[b][heads], ref, mag, slack, f"sequence {b}", R.P_BF16)
