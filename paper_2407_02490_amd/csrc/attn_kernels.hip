@@ -2998,7 +2998,7 @@ __global__ __launch_bounds__(256) void cache_prefix_kernel(CacheCall x) {
     const float l = st.l[nb] + __shfl_xor(st.l[nb], 32);
     if (rt * 256 + in_tile >= sh.rows) continue;
     const int64_t at = item * 256 + in_tile;
-    if (h == 0) sh.ml[at] = float2{st.m[nb], l};
+    if (h == 0) sh.ml[at] = float2{l == 0.f ? -INFINITY : st.m[nb], l};      // (all logits -inf: no reference for others)
     float *to = sh.o + at * D + 4 * h;
 #pragma unroll
     for (int db = 0; db < 4; ++db)

@@ -191,3 +191,29 @@ def test_large_values_behind_a_prefix_whose_logits_outgrow_their_first_tile(B, f
         heads = slice(0, 64, 8)                              # one query head of each group: all rows are alike
         ref, _, mag, slack = R.attention(qd[b][heads], kd[b], vd[b], 1 + b, 0, BIG, None, pk, pv)
         R.check_o(o[b][heads], ref, mag, slack, f"sequence {b}", R.P_BF16)
+
+
+@pytest.mark.parametrize("batch", [2, 10, 25, 40], ids=lambda b: f"{4 * b}-rows")
+def test_logits_of_minus_infinity_beside_very_low_ones(B, batch):  # noqa: F811
+    """Keys whose logits are -inf have no weight, also where they fill whole tiles and parts and all other logits lie at
+    -400 (base 2): the row is the softmax of those."""
+    P, hkv = 9000, 8
+    cache = cache_of(B, 90, batch, hkv, 32, [1 + i % 32 for i in range(batch)], weight=False)
+    prefix = cache_of(B, 91, 1, hkv, P + 20, [P], weight=False)
+    q = queries(90, batch, 4 * hkv, 1)
+    q[:] = q[:1, :1]
+    q[..., 0] = 1.0
+    d = q[0, 0, 0].float()
+    low = d * (-400.0 * float(np.log(2.0)) * float(np.sqrt(128.0)) / float(d @ d))
+    prefix.k[:, :, :P] = (0.1 * prefix.k[:, :, :P].float() + low).to(torch.bfloat16)
+    cache.k.copy_((0.1 * cache.k.float() + low).to(torch.bfloat16))
+    prefix.k[:, :, 1000:4000, 0] = float("-inf")
+    o = torch.full_like(q, float("nan"))
+    B.minf_prefix_attn(q, o, prefix, cache, workspace(B.minf_prefix_attn_workspace_bytes(q, prefix, cache)))
+    torch.cuda.synchronize()
+    left = np.r_[0:1000, 4000:P]
+    pk, pv = R.f64(prefix.k)[0][:, left], R.f64(prefix.v)[0][:, left]
+    qd, kd, vd = R.f64(q), R.f64(cache.k), R.f64(cache.v)
+    for b in (0, batch - 1):
+        ref, _, mag, slack = R.attention(qd[b][::4], kd[b], vd[b], 1 + b % 32, 0, BIG, None, pk, pv)
+        R.check_o(o[b][::4], ref, mag, slack, f"sequence {b}", R.P_BF16 if 4 * batch > 64 else R.P_TWO_BF16)
