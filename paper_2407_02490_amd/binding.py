@@ -415,14 +415,20 @@ def _cache_call(fn, cache, ws, stream, *args):
     _check(status)
 
 
+def _i32(n, most=2 ** 31 - 1):
+    """n for the library, whose integers have 32 bits: what lies beyond stays there (ctypes would cut the upper bits off)."""
+    return most if n > most else max(n, -1)
+
+
 def _weights(weights):
     assert weights in _WEIGHTS, 'weights: None, "set" or "add"'
     return _WEIGHTS[weights]
 
 
 def minf_cache_attn_workspace_bytes(q, cache, n_init=0, n_local=None, weights=None):
-    return int(lib().minf_cache_attn_workspace_bytes(ctypes.byref(_queries(q, None, cache, 0.0)), cache._ref, n_init,
-                                                     cache.capacity if n_local is None else n_local, _weights(weights)))
+    cap = cache.capacity
+    return int(lib().minf_cache_attn_workspace_bytes(ctypes.byref(_queries(q, None, cache, 0.0)), cache._ref, _i32(n_init, cap),
+                                                     cap if n_local is None else _i32(n_local, cap), _weights(weights)))
 
 
 def minf_prefix_attn_workspace_bytes(q, prefix, cache):
@@ -430,15 +436,16 @@ def minf_prefix_attn_workspace_bytes(q, prefix, cache):
 
 
 def minf_cache_evict_workspace_bytes(cache, keep):
-    return int(lib().minf_cache_evict_workspace_bytes(cache._ref, keep))
+    return int(lib().minf_cache_evict_workspace_bytes(cache._ref, _i32(keep)))
 
 
 def minf_cache_attn(q, o, cache, ws, n_init=0, n_local=None, weights=None, scale=0.0, stream=None):
     """o = attention of the newest tokens q against the cache, sink + sliding window (n_local=None: the
     whole cache); weights="set" / "add": cache.weight receives the attention weight of every slot.
     o may be q (not with weights of more than 16 rows per K/V head)."""
-    _cache_call(lib().minf_cache_attn, cache, ws, stream, ctypes.byref(_queries(q, o, cache, scale)), cache._ref, n_init,
-                cache.capacity if n_local is None else n_local, _weights(weights))
+    cap = cache.capacity
+    _cache_call(lib().minf_cache_attn, cache, ws, stream, ctypes.byref(_queries(q, o, cache, scale)), cache._ref, _i32(n_init, cap),
+                cap if n_local is None else _i32(n_local, cap), _weights(weights))
 
 
 def minf_prefix_attn(q, o, prefix, cache, ws, scale=0.0, stream=None):
@@ -455,4 +462,5 @@ def minf_cache_evict(cache, keep, ws, kept, to=None, n_init=0, n_recent=0, strea
     assert kept.dtype == torch.int32 and kept.is_contiguous() and kept.numel() == cache.batch * cache.n_kv_heads * keep, \
         "kept: int32 [B, Hkv, keep]"
     assert kept.device == cache.device and to.device == cache.device, "one device"
-    _cache_call(lib().minf_cache_evict, cache, ws, stream, cache._ref, n_init, n_recent, keep, to._ref, kept.data_ptr())
+    _cache_call(lib().minf_cache_evict, cache, ws, stream, cache._ref, _i32(n_init), _i32(n_recent), _i32(keep), to._ref,
+                kept.data_ptr())
