@@ -348,3 +348,54 @@ def test_evict_many_long_rows(B, shape, in_place):
         to = B.alloc_kv_cache(batch, heads, keep + 5)
         to.k.zero_(), to.v.zero_()
     evict_and_check(B, cache, keep, 17, 300, to)
+
+
+@pytest.mark.gpu
+def test_captured_calls_of_many_rows_and_long_rows(B):
+    """Attention of 100 rows with weights, a prefix of 160 rows and an eviction of long rows in one graph and one workspace,
+    one call after the other; replayed with other queries, weights and lengths between eager calls."""
+    own, pre = SHARED_CASES["100-rows"][1], SHARED_PREFIX_CASES["160-rows"][1]
+    q, kv, _, w = fill(own, 8)
+    pq, pkv, pp, pw = fill(pre, 9)
+    gen = torch.Generator("cuda").manual_seed(10)
+    cache, _ = own.caches(B, kv, None, w, "cuda")
+    branch, prefix = pre.caches(B, pkv, pp, pw, "cuda")
+    keep = 3001
+    long = B.KVCache(*(torch.empty(1, 8, 40000, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(2)),
+                     torch.tensor([40000], dtype=torch.int32, device="cuda"), torch.zeros(1, 8, 40000, device="cuda"))
+    need = max(B.minf_cache_attn_workspace_bytes(q, cache, weights="set"), B.minf_prefix_attn_workspace_bytes(pq, prefix, branch),
+               B.minf_cache_evict_workspace_bytes(long, keep))
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    to = [B.alloc_kv_cache(1, 8, keep) for _ in range(2)]
+    for t in to:
+        t.k.zero_(), t.v.zero_()
+    outs = [[torch.zeros_like(q), torch.zeros_like(pq), torch.zeros(1, 8, keep, dtype=torch.int32, device="cuda")] for _ in range(2)]
+
+    def step(i):
+        B.minf_cache_attn(q, outs[i][0], cache, ws, weights="set")
+        B.minf_prefix_attn(pq, outs[i][1], prefix, branch, ws)
+        B.minf_cache_evict(long, keep, ws, outs[i][2], to=to[i], n_init=5, n_recent=77)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(0)
+    for turn in range(4):
+        q.copy_(torch.randn(q.shape, generator=gen, device="cuda"))
+        pq.copy_(torch.randn(pq.shape, generator=gen, device="cuda"))
+        long.weight.exponential_(generator=gen)
+        long.lens.fill_([40000, 2000, 39999, 3002][turn])
+        cache.lens.copy_(cache.lens.roll(1))
+        prefix.lens.fill_([21001, 64, 0, 20000][turn])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs[0] + [w, to[0].k, to[0].v, to[0].weight, to[0].lens]]
+        w.zero_()
+        step(1)
+        torch.cuda.synchronize()
+        for b, n in enumerate(cache.lens.tolist()):          # slots behind the sequences are left as they were
+            got[3][b, :, n:] = 0.0
+        for i, (a, e) in enumerate(zip(got, outs[1] + [w, to[1].k, to[1].v, to[1].weight, to[1].lens])):
+            bits = {torch.bfloat16: torch.int16, torch.float32: torch.int32}.get(a.dtype, a.dtype)
+            assert torch.equal(a.view(bits), e.view(bits)), f"replay {turn}, output {i}"
