@@ -1543,7 +1543,8 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_emit_kernel(EvictCall x)
 // one sequence and K/V head (slices 0..3: K, 4..7: V), or its weights (the last slice), and walks them in ascending
 // order, a chunk into registers, then out: the kept slots ascend, so the rows of a later chunk, which are loaded
 // ahead, lie behind everything that this chunk overwrites.  Into another cache whole rows (slices K, V, weights) in
-// any order.
+// any order.  (8 heads, 16K of 1M and 64K of 128K slots kept: 24 and 105 us into another cache, at 5.4 TB/s; in place 194
+// and 756, a chain of 64 and 256 dependent chunks on 72 workgroups.)
 constexpr int MOVE_ROWS = 4;                                     // a thread, at a time
 template <bool IN_PLACE>
 __global__ __launch_bounds__(256) void cache_move_kernel(EvictCall x) {
